@@ -363,6 +363,83 @@ bls_status_t bls_interact(const void *x, int ldx, const float *pooled, int rows,
                           void *cuda_stream);
 bls_status_t bls_mlp_status(bls_mlp_t *handle, void *cuda_stream);
 
+/* ---- the expert stage: a mixture of expert layers next to the dense stages ----
+ * A request's rows (tokens) go to k experts each, as row IDs go to the ranks that own them: slots
+ * are sorted by expert, rows are moved there, every expert's layer answers its rows (weights in
+ * 4 bits, see below), and the answers come back as a weighted sum.  The calls are stateless: all
+ * buffers are DEVICE memory of the caller, work is enqueued on cuda_stream, nothing synchronises.
+ *
+ * expert int32 [tokens][k]: the expert of every slot.  An ID outside [0, n_experts) names no expert
+ * held here (a masked token, a dropped slot, an expert of another rank): that slot is left out.
+ * tokens may be 0; tokens * k and rows at most 2^30; 1 <= k <= 1024, 1 <= n_experts <= 1024.
+ *   bls_moe_bytes    workspace of bls_moe_route (256-byte aligned; may be 0)
+ *   bls_moe_route    stable sort of the kept slots by expert:
+ *                    offsets int32 [n_experts + 1]  first sorted position of every expert, then the number of kept slots
+ *                    order   int32 [tokens * k]     slot t * k + i at every sorted position, -1 past offsets[n_experts]
+ *                    place   int32 [tokens][k]      sorted position of every slot, -1 when it is left out
+ *   bls_moe_dispatch y[place[t][i]] = x[t]; rows of y from offsets[n_experts] on are set to 0.
+ *                    Its gradient with respect to x is bls_moe_combine without weights.
+ *   bls_moe_combine  out[t] = sum over i of w[t][i] * y[place[t][i]], fp32 sum in the order of i, rounded
+ *                    once; w fp32 [tokens][k] or NULL (all 1).  Slots left out add nothing, whatever w
+ *                    holds there; a token without slots gives 0.
+ *   bls_moe_combine_grad  of bls_moe_combine: dy[place[t][i]] = w[t][i] * dout[t] (rows from
+ *                    offsets[n_experts] on: 0) and dw[t][i] = <dout[t], y[place[t][i]]> in fp32 (0 for
+ *                    slots left out).  dw may be NULL (then y is not read), w as above.
+ * x, y, out, dout, dy have one dtype (BLS_F32, BLS_BF16, BLS_F16), dim columns and row pitches ld*
+ * >= dim in elements; `rows` is the number of rows of y and dy (a place at or past it is treated as
+ * left out); outputs must not overlap inputs. */
+bls_status_t bls_moe_bytes(int64_t tokens, int k, int n_experts, size_t *bytes /*host*/);
+bls_status_t bls_moe_route(const int32_t *expert, int64_t tokens, int k, int n_experts, int32_t *order, int32_t *place,
+                           int32_t *offsets, void *workspace, size_t bytes, void *cuda_stream);
+bls_status_t bls_moe_dispatch(const void *x, int64_t ldx, int dtype, const int32_t *place, const int32_t *offsets,
+                              int n_experts, int64_t tokens, int k, int dim, void *y, int64_t ldy, int64_t rows,
+                              void *cuda_stream);
+bls_status_t bls_moe_combine(const void *y, int64_t ldy, int64_t rows, int dtype, const int32_t *place, const float *w,
+                             int64_t tokens, int k, int dim, void *out, int64_t ldo, void *cuda_stream);
+bls_status_t bls_moe_combine_grad(const void *dout, int64_t ldd, const void *y, int64_t ldy, int64_t rows, int dtype,
+                                  const int32_t *place, const int32_t *offsets, int n_experts, const float *w,
+                                  int64_t tokens, int k, int dim, void *dy, int64_t lddy, float *dw, void *cuda_stream);
+
+/* Linear layers with weights in 4 bits and one scale per group of inputs.  E matrices (experts; 1
+ * for a plain layer) of N outputs x K inputs; a weight is (q - z) * s with q in 0..15, s (bfloat16)
+ * and z (0..15; 8 where no zero points are kept) of its group of `group` = 32, 64 or 128 inputs.
+ * Storage, with NT = ceil(N / 128), KT = ceil(K / 128), 16-byte aligned:
+ *   q      uint8 [E][NT][KT][128][64]: tiles of 128 outputs x 128 inputs.  In the 64 bytes of output
+ *          r the 16-byte piece at position p is quarter t = p ^ ((r >> 1) & 3); its 32-bit word b holds
+ *          inputs 32 b + 8 t + i, i = 0..7, input i in bits 4 j .. 4 j + 3 with j = i / 2 + 4 (i mod 2)
+ *   scale  bfloat16 [E][KT * 128 / group][NT * 128]
+ *   zero   uint8, shaped like scale, or NULL
+ * Entries past N and K hold scale 0 (and any finite q).  The piece order lets one thread take a whole row
+ * from shared memory without bank conflicts, the word and bit order gives pairs of neighbouring
+ * inputs from one shift and one mask, and any group of 32 inputs is one word of each quarter.
+ *   bls_w4_sizes       bytes of q and elements of scale (and of zero)
+ *   bls_w4_quantize    w [E][N][K] (dtype, row pitch ldw, matrices N * ldw apart) -> q, scale, zero.
+ *                      zero NULL (symmetric): s = bf16(max|w| / 7), q = clamp(rint(w / s), -8, 7) + 8.
+ *                      With zero points, lo = min(w, 0), hi = max(w, 0): s = bf16((hi - lo) / 15),
+ *                      z = clamp(rint(-lo / s), 0, 15), q = clamp(rint(w / s) + z, 0, 15).  s = 0 gives
+ *                      q = z; a NaN or an infinity makes its whole group NaN.  Quotients are fp32.
+ *   bls_w4_dequantize  the weights (q - z) * s in fp32, rounded once to dtype
+ *   bls_w4_bytes       workspace of bls_w4_linear (256-byte aligned; may be 0)
+ *   bls_w4_linear      y[r][n] = act(bias[e][n] + sum over groups of s * sum of (q - z) * x[r][..]), e = the
+ *                      matrix of row r: rows offsets[e] .. offsets[e + 1] - 1 (int32 [E + 1], as bls_moe_route
+ *                      gives them; NULL with E = 1: all rows).  Rows from offsets[E] on are set to 0.
+ *                      x BLS_BF16 or BLS_F16 [rows][ldx], y [rows][ldy] of y_dtype (any of the three); bias fp32
+ *                      [E][N] or NULL; act 0 none, 1 ReLU, 2 logistic function.  q - z is exact in
+ *                      x's type, products are summed in fp32 group by group and scaled in fp32: weights
+ *                      are never rounded.  rows may be 0.
+ *                      status: one int32 of device memory, zeroed by the caller before the first call; a
+ *                      bounded wait that gives up sets bit 8 in it (BLS_ETIMEOUT) and y is then incomplete */
+bls_status_t bls_w4_sizes(int E, int N, int K, int group, int64_t *q_bytes /*host*/, int64_t *scale_elems /*host*/);
+bls_status_t bls_w4_quantize(const void *w, int dtype, int64_t ldw, int E, int N, int K, int group, uint8_t *q, void *scale,
+                             uint8_t *zero, void *cuda_stream);
+bls_status_t bls_w4_dequantize(const uint8_t *q, const void *scale, const uint8_t *zero, int E, int N, int K, int group,
+                               void *w, int dtype, int64_t ldw, void *cuda_stream);
+bls_status_t bls_w4_bytes(int E, int N, int K, int64_t rows, size_t *bytes /*host*/);
+bls_status_t bls_w4_linear(const uint8_t *q, const void *scale, const uint8_t *zero, int E, int N, int K, int group,
+                           const void *x, int x_dtype, int64_t ldx, int64_t rows, const int32_t *offsets,
+                           const float *bias, int act, void *y, int y_dtype, int64_t ldy, void *workspace, size_t bytes,
+                           int32_t *status, void *cuda_stream);
+
 /* ---- allocation-free router (the paper has no counterpart: this entry point
  * exists for deployment reasons only) ----
  * Step (1) for table-wise round-robin placement, for callers that cannot

@@ -28,7 +28,8 @@ EXPORTS = ["bls_plan_bytes", "bls_plan", "bls_destroy", "bls_route", "bls_lookup
            "bls_profile", "bls_profile_read", "bls_set_tuning", "bls_route_table_rr_static",
            "bls_set_random_stall", "bls_set_ring", "bls_timeline", "bls_set_poison", "bls_set_overlap", "bls_set_fused", "bls_a2a_bytes", "bls_a2a_create", "bls_a2a_destroy", "bls_a2a_post", "bls_a2a_wait",
            "bls_a2a_status", "bls_mlp_bytes", "bls_mlp_create", "bls_mlp_destroy", "bls_mlp_forward", "bls_interact",
-           "bls_mlp_status", "bls_hot_bytes", "bls_hot_attach", "bls_hot_observe", "bls_hot_build", "bls_hot_view"]
+           "bls_mlp_status", "bls_moe_bytes", "bls_moe_route", "bls_moe_dispatch", "bls_moe_combine", "bls_moe_combine_grad",
+           "bls_w4_sizes", "bls_w4_quantize", "bls_w4_dequantize", "bls_w4_bytes", "bls_w4_linear", "bls_hot_bytes", "bls_hot_attach", "bls_hot_observe", "bls_hot_build", "bls_hot_view"]
 
 
 class BlsError(RuntimeError):
@@ -63,6 +64,17 @@ def lib():
         _lib.bls_strerror.argtypes = [C.c_int]
         # the call of the inner loop: with declared argument types plain Python integers can be passed
         _lib.bls_step.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        p, i, l = C.c_void_p, C.c_int, C.c_int64
+        _lib.bls_moe_bytes.argtypes = [l, i, i, p]
+        _lib.bls_moe_route.argtypes = [p, l, i, i, p, p, p, p, C.c_size_t, p]
+        _lib.bls_moe_dispatch.argtypes = [p, l, i, p, p, i, l, i, i, p, l, l, p]
+        _lib.bls_moe_combine.argtypes = [p, l, l, i, p, p, l, i, i, p, l, p]
+        _lib.bls_moe_combine_grad.argtypes = [p, l, p, l, l, i, p, p, i, p, l, i, i, p, l, p, p]
+        _lib.bls_w4_sizes.argtypes = [i, i, i, i, p, p]
+        _lib.bls_w4_quantize.argtypes = [p, i, l, i, i, i, i, p, p, p, p]
+        _lib.bls_w4_dequantize.argtypes = [p, p, p, i, i, i, i, p, i, l, p]
+        _lib.bls_w4_bytes.argtypes = [i, i, i, l, p]
+        _lib.bls_w4_linear.argtypes = [p, p, p, i, i, i, i, p, i, l, l, p, p, i, p, i, l, p, C.c_size_t, p, p]
     return _lib
 
 
@@ -440,3 +452,199 @@ def bls_interact(x: torch.Tensor, pooled: torch.Tensor, r: torch.Tensor, stream:
     T = pooled.numel() // (rows * D)
     _check(lib().bls_interact(C.c_void_p(x.data_ptr()), x.stride(0), C.c_void_p(pooled.data_ptr()), rows, T, D,
                               C.c_void_p(r.data_ptr()), r.stride(0), _stream_ptr(stream)), "bls_interact")
+
+
+# ---- the expert stage ----
+
+def _on(stream: Optional[torch.cuda.Stream], like: torch.Tensor) -> int:
+    """Handle of the stream that a call on `like` is enqueued on."""
+    return stream.cuda_stream if stream is not None else torch.cuda.current_stream(like.device).cuda_stream
+
+
+def _scratch(n: int, stream: Optional[torch.cuda.Stream], like: torch.Tensor) -> torch.Tensor:
+    """n bytes for one call, allocated on the call's own stream so that later work there cannot overtake it."""
+    if stream is None:
+        return torch.empty(n, dtype=torch.uint8, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=torch.uint8, device=like.device)
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _rows(t: torch.Tensor, name: str, shape, dtype: Optional[torch.dtype] = None):
+    """A matrix whose rows are contiguous (any row pitch), of one type, on a GPU."""
+    _need(t.is_cuda and t.dim() == 2 and tuple(t.shape) == tuple(shape) and (t.shape[1] < 2 or t.stride(1) == 1) and
+          (t.shape[0] < 2 or t.stride(0) >= t.shape[1]) and (t.dtype == dtype if dtype else t.dtype in _DTYPE),
+          f"{name}: expected a CUDA matrix {tuple(shape)}{' of ' + str(dtype) if dtype else ''} with contiguous rows")
+
+
+def _pitch(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _flat(t: Optional[torch.Tensor], name: str, shape, dtype: torch.dtype):
+    """A contiguous tensor of one shape and type on a GPU; its address (None stays None)."""
+    if t is None:
+        return None
+    _need(t.is_cuda and t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
+          f"{name}: expected a contiguous CUDA tensor {tuple(shape)} of {dtype}")
+    return t.data_ptr()
+
+
+def bls_moe_route(expert: torch.Tensor, n_experts: int, order: torch.Tensor, place: torch.Tensor, offsets: torch.Tensor,
+                  stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Stable sort of the slots expert int32 [n][k] by expert; IDs outside [0, n_experts) leave their slot out.
+    order int32 [n*k], place int32 [n][k], offsets int32 [n_experts+1] are written."""
+    _need(expert.dim() == 2, "expert: expected [tokens][k]")
+    n, k = expert.shape
+    i32 = torch.int32
+    args = (_flat(expert, "expert", (n, k), i32), n, k, n_experts, _flat(order, "order", (n * k,), i32),
+            _flat(place, "place", (n, k), i32), _flat(offsets, "offsets", (n_experts + 1,), i32))
+    nbytes = C.c_size_t(0)
+    _check(lib().bls_moe_bytes(n, k, n_experts, C.byref(nbytes)), "bls_moe_bytes")
+    ws = _scratch(nbytes.value, stream, expert) if nbytes.value else None
+    _check(_lib.bls_moe_route(*args, ws.data_ptr() if ws is not None else None, nbytes.value, _on(stream, expert)), "bls_moe_route")
+
+
+def bls_moe_dispatch(x: torch.Tensor, place: torch.Tensor, offsets: torch.Tensor, y: torch.Tensor,
+                     stream: Optional[torch.cuda.Stream] = None) -> None:
+    """y[place[t][i]] = x[t]; the rows of y from offsets[-1] on become 0.  x [n][D], y [rows][D] of one type."""
+    _need(place.dim() == 2 and y.dim() == 2 and x.dim() == 2, "x, y and place are matrices")
+    n, k = place.shape
+    D = x.shape[1]
+    _rows(x, "x", (n, D))
+    _rows(y, "y", (y.shape[0], D), x.dtype)
+    _check(lib().bls_moe_dispatch(x.data_ptr(), _pitch(x), _DTYPE[x.dtype], _flat(place, "place", (n, k), torch.int32),
+                                  _flat(offsets, "offsets", (offsets.numel(),), torch.int32), offsets.numel() - 1, n, k, D,
+                                  y.data_ptr(), _pitch(y), y.shape[0], _on(stream, x)), "bls_moe_dispatch")
+
+
+def bls_moe_combine(y: torch.Tensor, place: torch.Tensor, w: Optional[torch.Tensor], out: torch.Tensor,
+                    stream: Optional[torch.cuda.Stream] = None) -> None:
+    """out[t] = sum over i of w[t][i] * y[place[t][i]] (w fp32 [n][k] or None: all 1).  y [rows][D], out [n][D] of one type."""
+    _need(place.dim() == 2 and y.dim() == 2 and out.dim() == 2, "y, out and place are matrices")
+    n, k = place.shape
+    D = out.shape[1]
+    _rows(out, "out", (n, D))
+    _rows(y, "y", (y.shape[0], D), out.dtype)
+    _check(lib().bls_moe_combine(y.data_ptr(), _pitch(y), y.shape[0], _DTYPE[y.dtype], _flat(place, "place", (n, k), torch.int32),
+                                 _flat(w, "w", (n, k), torch.float32), n, k, D, out.data_ptr(), _pitch(out), _on(stream, y)),
+           "bls_moe_combine")
+
+
+def bls_moe_combine_grad(dout: torch.Tensor, y: Optional[torch.Tensor], place: torch.Tensor, offsets: torch.Tensor,
+                         w: Optional[torch.Tensor], dy: torch.Tensor, dw: Optional[torch.Tensor] = None,
+                         stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Gradients of bls_moe_combine: dy[place[t][i]] = w[t][i] * dout[t] and, if wanted, dw[t][i] = <dout[t], y[place[t][i]]>."""
+    _need(place.dim() == 2 and dout.dim() == 2 and dy.dim() == 2, "dout, dy and place are matrices")
+    n, k = place.shape
+    D, rows = dout.shape[1], dy.shape[0]
+    _rows(dout, "dout", (n, D))
+    _rows(dy, "dy", (rows, D), dout.dtype)
+    _need(dw is None or y is not None, "dw needs y")
+    if dw is not None:
+        _rows(y, "y", (rows, D), dout.dtype)
+    else:
+        y = None
+    _check(lib().bls_moe_combine_grad(dout.data_ptr(), _pitch(dout), y.data_ptr() if y is not None else None,
+                                      _pitch(y) if y is not None else D, rows, _DTYPE[dout.dtype],
+                                      _flat(place, "place", (n, k), torch.int32),
+                                      _flat(offsets, "offsets", (offsets.numel(),), torch.int32), offsets.numel() - 1,
+                                      _flat(w, "w", (n, k), torch.float32), n, k, D, dy.data_ptr(), _pitch(dy),
+                                      _flat(dw, "dw", (n, k), torch.float32), _on(stream, dout)), "bls_moe_combine_grad")
+
+
+class W4:
+    """E matrices [N][K] in 4 bits with group scales: the three tensors of the storage format (include/bls.h)."""
+    __slots__ = ("q", "scale", "zero", "E", "N", "K", "group", "_ptrs")
+
+    def __init__(self, q: torch.Tensor, scale: torch.Tensor, zero: Optional[torch.Tensor], N: int, K: int, group: int):
+        nt, kt = (N + 127) // 128, (K + 127) // 128
+        _need(group in (32, 64, 128) and N >= 1 and K >= 1 and q.dim() == 5, "W4: bad sizes")
+        E = q.shape[0]
+        shape = (E, kt * 128 // group, nt * 128)
+        self._ptrs = (_flat(q, "q", (E, nt, kt, 128, 64), torch.uint8), _flat(scale, "scale", shape, torch.bfloat16),
+                      _flat(zero, "zero", shape, torch.uint8), E, N, K, group)
+        self.q, self.scale, self.zero, self.E, self.N, self.K, self.group = q, scale, zero, E, N, K, group
+
+
+def bls_w4_sizes(E: int, N: int, K: int, group: int):
+    """(bytes of q, elements of scale)."""
+    a, b = C.c_int64(0), C.c_int64(0)
+    _check(lib().bls_w4_sizes(E, N, K, group, C.byref(a), C.byref(b)), "bls_w4_sizes")
+    return a.value, b.value
+
+
+def _matrices(w: torch.Tensor, name: str):
+    """(E, N, K, row pitch) of weights [E][N][K] or [N][K] with contiguous rows, matrices N pitches apart."""
+    _need(w.is_cuda and w.dtype in _DTYPE and w.dim() in (2, 3) and w.numel() > 0, f"{name}: expected CUDA weights [N][K] or [E][N][K]")
+    E, (N, K) = (w.shape[0] if w.dim() == 3 else 1), w.shape[-2:]
+    ld = w.stride(-2) if N > 1 else (w.stride(0) if E > 1 else K)
+    _need((K < 2 or w.stride(-1) == 1) and ld >= K and (E < 2 or w.stride(0) == N * ld), f"{name}: rows must be contiguous, matrices N rows apart")
+    return E, N, K, ld
+
+
+def bls_w4_quantize(w: torch.Tensor, group: int = 128, symmetric: bool = True, stream: Optional[torch.cuda.Stream] = None) -> W4:
+    """Weights [E][N][K] or [N][K] in 4 bits with one scale (and, unless symmetric, one zero point) per `group` inputs."""
+    E, N, K, ld = _matrices(w, "w")
+    _need(group in (32, 64, 128), "group: 32, 64 or 128")
+    nt, kt = (N + 127) // 128, (K + 127) // 128
+    ns = E * kt * (128 // group) * nt * 128
+    nq = E * nt * kt * 8192
+    buf = _scratch(nq + ns * (2 if symmetric else 3), stream, w)           # one allocation: q, scale, zero
+    shape = (E, kt * 128 // group, nt * 128)
+    t = W4(buf[:nq].view(E, nt, kt, 128, 64), buf[nq:nq + 2 * ns].view(torch.bfloat16).view(shape),
+           None if symmetric else buf[nq + 2 * ns:].view(shape), N, K, group)
+    _check(lib().bls_w4_quantize(w.data_ptr(), _DTYPE[w.dtype], ld, E, N, K, group, t._ptrs[0], t._ptrs[1], t._ptrs[2],
+                                 _on(stream, w)), "bls_w4_quantize")
+    return t
+
+
+def bls_w4_dequantize(w4: W4, w: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """w [E][N][K] (or [N][K] with E = 1) = (q - z) * s, rounded once to w's type."""
+    E, N, K, ld = _matrices(w, "w")
+    _need((E, N, K) == (w4.E, w4.N, w4.K), f"w: expected {(w4.E, w4.N, w4.K)}")
+    _check(lib().bls_w4_dequantize(*w4._ptrs, w.data_ptr(), _DTYPE[w.dtype], ld, _on(stream, w)), "bls_w4_dequantize")
+
+
+_w4_status_word = {}                         # device -> int32 [1], zeroed once: bounded waits that gave up are latched here
+
+
+def _status_word(device: torch.device) -> torch.Tensor:
+    t = _w4_status_word.get(device)
+    if t is None:
+        t = _w4_status_word[device] = torch.zeros(1, dtype=torch.int32, device=device)
+        torch.cuda.synchronize(device)       # once: calls on any stream may use it from here on
+    return t
+
+
+def bls_w4_status(device="cuda") -> int:
+    """Synchronises the device; BLS_ETIMEOUT if a bounded wait inside a 4-bit product gave up."""
+    device = torch.device(device)
+    if device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    torch.cuda.synchronize(device)
+    return BLS_ETIMEOUT if int(_status_word(device).item()) & 8 else BLS_OK
+
+
+def bls_w4_linear(w4: W4, x: torch.Tensor, y: torch.Tensor, offsets: Optional[torch.Tensor] = None,
+                  bias: Optional[torch.Tensor] = None, act: int = 0, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """y = act(x W^T + bias), row by row with the matrix that offsets int32 [E+1] gives it (None with E = 1); rows from
+    offsets[-1] on become 0.  x [rows][K] bf16 or f16, y [rows][N] bf16, f16 or fp32, bias fp32 [E][N];
+    act 0 none, 1 ReLU, 2 logistic function."""
+    _need(x.dim() == 2, "x is a matrix")
+    rows = x.shape[0]
+    _rows(x, "x", (rows, w4.K))
+    _rows(y, "y", (rows, w4.N))
+    _need(x.dtype != torch.float32, "x: expected bf16 or f16")
+    _need(offsets is not None or w4.E == 1, "offsets are needed with more than one matrix")
+    nbytes = C.c_size_t(0)
+    _check(lib().bls_w4_bytes(w4.E, w4.N, w4.K, rows, C.byref(nbytes)), "bls_w4_bytes")
+    ws = _scratch(nbytes.value, stream, x) if nbytes.value else None
+    _check(_lib.bls_w4_linear(*w4._ptrs, x.data_ptr(), _DTYPE[x.dtype], _pitch(x), rows,
+                              _flat(offsets, "offsets", (w4.E + 1,), torch.int32), _flat(bias, "bias", (w4.E, w4.N), torch.float32),
+                              act, y.data_ptr(), _DTYPE[y.dtype], _pitch(y), ws.data_ptr() if ws is not None else None, nbytes.value,
+                              _status_word(x.device).data_ptr(), _on(stream, x)), "bls_w4_linear")

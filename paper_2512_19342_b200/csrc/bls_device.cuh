@@ -24,12 +24,13 @@ __device__ __forceinline__ void stream_order_enter()
 }
 
 template <class... Params, class... Args>
-static inline cudaError_t launch_serialised(void (*kernel)(Params...), dim3 grid, dim3 block, cudaStream_t stream,
-                                            Args... args)
+static inline cudaError_t launch_serialised_smem(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem,
+                                                 cudaStream_t stream, Args... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -37,6 +38,13 @@ static inline cudaError_t launch_serialised(void (*kernel)(Params...), dim3 grid
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
+}
+
+template <class... Params, class... Args>
+static inline cudaError_t launch_serialised(void (*kernel)(Params...), dim3 grid, dim3 block, cudaStream_t stream,
+                                            Args... args)
+{
+    return launch_serialised_smem(kernel, grid, block, 0, stream, args...);
 }
 
 __device__ __forceinline__ void flag(const BlsParams &p, int bit) { atomicOr(&p.dev->status, bit); }

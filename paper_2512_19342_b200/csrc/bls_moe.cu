@@ -1,0 +1,322 @@
+// The movements of an expert stage: slots sorted by expert, rows moved to their experts and
+// back as a weighted sum, and the gradients of both moves.
+//
+// Routing is a stable counting sort.  A tile of consecutive slots is counted per warp, an
+// exclusive scan over (expert, tile, warp) gives every warp its first position for every
+// expert, and inside a warp the position of a slot is the number of lower lanes with the same
+// expert (match.any).  Positions depend on scans only: the result is the unique stable sort, the
+// same in every run.
+//
+// The moves are bound by memory: every row is read and written once, sums are fp32.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include "bls_device.cuh"
+#include "bls_internal.h"
+
+namespace {
+
+constexpr int ROUTE_THREADS = 1024;
+constexpr int ROUTE_WARPS = ROUTE_THREADS / 32;
+constexpr int MOE_MAX_EXPERTS = 1024;
+constexpr int MOVE_THREADS = 256;
+
+// Inclusive scan over the block of one value per thread; scratch holds 32 words.
+__device__ __forceinline__ int block_scan(int v, int *scratch)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    #pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(~0u, v, d);
+        if (lane >= d) v += o;
+    }
+    if (lane == 31) scratch[warp] = v;
+    __syncthreads();
+    if (warp == 0) {
+        int s = scratch[lane];
+        #pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(~0u, s, d);
+            if (lane >= d) s += o;
+        }
+        scratch[lane] = s;
+    }
+    __syncthreads();
+    return v + (warp ? scratch[warp - 1] : 0);
+}
+
+// One block sorts all slots.  hist [ROUTE_WARPS][E]: counts, then first positions, of every warp.
+__global__ void __launch_bounds__(ROUTE_THREADS) bls_moe_route_kernel(const int *expert, int n, int E, int *order, int *place, int *offsets)
+{
+    stream_order_enter();
+    extern __shared__ int hist[];
+    __shared__ int scratch[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int i = threadIdx.x; i < ROUTE_WARPS * E; i += ROUTE_THREADS) hist[i] = 0;
+    __syncthreads();
+    const int per = ((n + ROUTE_WARPS - 1) / ROUTE_WARPS + 31) & ~31;         // consecutive slots of a warp
+    const int lo = min((long long)warp * per, (long long)n), hi = min((long long)lo + per, (long long)n);
+    int *mine = hist + warp * E;
+    for (int i = lo; i < hi; i += 32) {
+        const int e = i + lane < hi ? expert[i + lane] : -1;
+        const bool kept = (unsigned)e < (unsigned)E;
+        const unsigned same = __match_any_sync(~0u, kept ? e : -1);
+        if (kept && lane == __ffs(same) - 1) mine[e] += __popc(same);
+        __syncwarp();
+    }
+    __syncthreads();
+    int total = 0;
+    if (threadIdx.x < E)
+        for (int w = 0; w < ROUTE_WARPS; w++) total += hist[w * E + threadIdx.x];
+    const int incl = block_scan(total, scratch);
+    if (threadIdx.x < E) {
+        int at = incl - total;
+        offsets[threadIdx.x] = at;
+        if (threadIdx.x == E - 1) offsets[E] = incl;
+        for (int w = 0; w < ROUTE_WARPS; w++) {
+            const int c = hist[w * E + threadIdx.x];
+            hist[w * E + threadIdx.x] = at;
+            at += c;
+        }
+    }
+    __syncthreads();
+    for (int i = lo; i < hi; i += 32) {
+        const int e = i + lane < hi ? expert[i + lane] : -1;
+        const bool kept = (unsigned)e < (unsigned)E;
+        const unsigned same = __match_any_sync(~0u, kept ? e : -1);
+        const int first = kept ? mine[e] : 0;
+        __syncwarp();
+        if (kept) {
+            const int at = first + __popc(same & ((1u << lane) - 1));
+            order[at] = i + lane;
+            place[i + lane] = at;
+            if (lane == __ffs(same) - 1) mine[e] = first + __popc(same);
+        } else if (i + lane < hi) {
+            place[i + lane] = -1;
+        }
+        __syncwarp();
+    }
+    // scratch[31] still holds the number of kept slots
+    for (int i = scratch[31] + threadIdx.x; i < n; i += ROUTE_THREADS) order[i] = -1;
+}
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
+template <class T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
+
+// V elements of T that move as one piece (16 bytes, or one element where rows do not allow it).
+template <class T, int V> struct alignas(sizeof(T) * V) Piece { T v[V]; };
+
+struct MoveArgs {
+    const void *a;              // dispatch: x; combine: y; gradient: dout
+    const void *b;              // gradient: y
+    void *o;                    // dispatch: y; combine: out; gradient: dy
+    long long lda, ldb, ldo;
+    const int *place, *total;   // total: number of sorted rows (device)
+    const float *w;
+    float *dw;
+    long long tokens, rows;
+    int k, pieces;              // pieces of a row
+};
+
+// Sets the rows of o from *total on to zero; the blocks of the grid share them.
+template <class T, int V>
+__device__ __forceinline__ void zero_tail(const MoveArgs &m)
+{
+    const long long first = max(0, *m.total);
+    for (long long i = first * m.pieces + (long long)blockIdx.x * blockDim.x + threadIdx.x; i < m.rows * m.pieces; i += (long long)gridDim.x * blockDim.x) {
+        Piece<T, V> z;
+        #pragma unroll
+        for (int c = 0; c < V; c++) z.v[c] = from_f<T>(0.f);
+        *(Piece<T, V> *)((T *)m.o + i / m.pieces * m.ldo + i % m.pieces * V) = z;
+    }
+}
+
+// One thread per piece of a token: read once, written to the token's k places.
+template <class T, int V>
+__global__ void __launch_bounds__(MOVE_THREADS) bls_moe_dispatch_kernel(MoveArgs m)
+{
+    stream_order_enter();
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < m.tokens * m.pieces; i += (long long)gridDim.x * blockDim.x) {
+        const long long t = i / m.pieces;
+        const long long c = i % m.pieces * V;
+        const Piece<T, V> p = *(const Piece<T, V> *)((const T *)m.a + t * m.lda + c);
+        for (int j = 0; j < m.k; j++) {
+            const int at = m.place[t * m.k + j];
+            if (at >= 0 && at < m.rows) *(Piece<T, V> *)((T *)m.o + at * m.ldo + c) = p;
+        }
+    }
+    zero_tail<T, V>(m);
+}
+
+template <class T, int V>
+__global__ void __launch_bounds__(MOVE_THREADS) bls_moe_combine_kernel(MoveArgs m)
+{
+    stream_order_enter();
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < m.tokens * m.pieces; i += (long long)gridDim.x * blockDim.x) {
+        const long long t = i / m.pieces;
+        const long long c = i % m.pieces * V;
+        float acc[V];
+        #pragma unroll
+        for (int e = 0; e < V; e++) acc[e] = 0.f;
+        for (int j = 0; j < m.k; j++) {
+            const int at = m.place[t * m.k + j];
+            if (at < 0 || at >= m.rows) continue;
+            const float w = m.w ? m.w[t * m.k + j] : 1.f;
+            const Piece<T, V> p = *(const Piece<T, V> *)((const T *)m.a + at * m.lda + c);
+            #pragma unroll
+            for (int e = 0; e < V; e++) acc[e] = fmaf(w, to_f(p.v[e]), acc[e]);
+        }
+        Piece<T, V> r;
+        #pragma unroll
+        for (int e = 0; e < V; e++) r.v[e] = from_f<T>(acc[e]);
+        *(Piece<T, V> *)((T *)m.o + t * m.ldo + c) = r;
+    }
+}
+
+// One warp per slot: dy = w * dout and dw = <dout, y> in one pass over the row.
+template <class T, int V>
+__global__ void __launch_bounds__(MOVE_THREADS) bls_moe_combine_grad_kernel(MoveArgs m)
+{
+    stream_order_enter();
+    const int lane = threadIdx.x & 31;
+    const long long warps = (long long)gridDim.x * (blockDim.x >> 5);
+    for (long long s = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5); s < m.tokens * m.k; s += warps) {
+        const int at = m.place[s];
+        const bool kept = at >= 0 && at < m.rows;
+        float dot = 0.f;
+        if (kept) {
+            const float w = m.w ? m.w[s] : 1.f;
+            const T *d = (const T *)m.a + s / m.k * m.lda;
+            for (int i = lane; i < m.pieces; i += 32) {
+                const Piece<T, V> g = *(const Piece<T, V> *)(d + i * V);
+                if (m.dw) {
+                    const Piece<T, V> y = *(const Piece<T, V> *)((const T *)m.b + at * m.ldb + i * V);
+                    #pragma unroll
+                    for (int e = 0; e < V; e++) dot = fmaf(to_f(g.v[e]), to_f(y.v[e]), dot);
+                }
+                Piece<T, V> r;
+                #pragma unroll
+                for (int e = 0; e < V; e++) r.v[e] = from_f<T>(w * to_f(g.v[e]));
+                *(Piece<T, V> *)((T *)m.o + at * m.ldo + i * V) = r;
+            }
+        }
+        if (m.dw) {
+            #pragma unroll
+            for (int o = 16; o; o >>= 1) dot += __shfl_xor_sync(~0u, dot, o);
+            if (lane == 0) m.dw[s] = kept ? dot : 0.f;
+        }
+    }
+    zero_tail<T, V>(m);
+}
+
+bool whole_pieces(const void *p, long long ld, int dim, int elem)
+{
+    return ((uintptr_t)p & 15) == 0 && (ld * elem) % 16 == 0 && (dim * (long long)elem) % 16 == 0;
+}
+
+enum { MOVE_DISPATCH, MOVE_COMBINE, MOVE_GRAD };
+
+template <class T, int V>
+cudaError_t launch_move_v(int what, MoveArgs m, int dim, cudaStream_t s)
+{
+    m.pieces = dim / V;
+    const long long items = what == MOVE_GRAD ? m.tokens * m.k * 32 : m.tokens * m.pieces;
+    const unsigned blocks = (unsigned)max(1ll, min((items + MOVE_THREADS - 1) / MOVE_THREADS, 148ll * 32));
+    void (*kernel)(MoveArgs) = what == MOVE_DISPATCH ? bls_moe_dispatch_kernel<T, V> :
+                               what == MOVE_COMBINE ? bls_moe_combine_kernel<T, V> : bls_moe_combine_grad_kernel<T, V>;
+    return launch_serialised(kernel, dim3(blocks), dim3(MOVE_THREADS), s, m);
+}
+
+bls_status_t launch_move(int what, const MoveArgs &m, int dtype, int dim, bool whole, cudaStream_t s)
+{
+    cudaError_t e;
+    switch (dtype) {
+    case BLS_F32: e = whole ? launch_move_v<float, 4>(what, m, dim, s) : launch_move_v<float, 1>(what, m, dim, s); break;
+    case BLS_BF16: e = whole ? launch_move_v<__nv_bfloat16, 8>(what, m, dim, s) : launch_move_v<__nv_bfloat16, 1>(what, m, dim, s); break;
+    default: e = whole ? launch_move_v<__half, 8>(what, m, dim, s) : launch_move_v<__half, 1>(what, m, dim, s); break;
+    }
+    return e == cudaSuccess ? BLS_OK : BLS_ECUDA;
+}
+
+bool slots_ok(int64_t tokens, int k, int n_experts)
+{
+    return tokens >= 0 && k >= 1 && k <= 1024 && n_experts >= 1 && n_experts <= MOE_MAX_EXPERTS && tokens <= (1 << 30) / k;
+}
+bool move_ok(int dtype, int64_t tokens, int k, int dim, int64_t rows, int64_t ld0, int64_t ld1)
+{
+    return dtype >= 0 && dtype <= 2 && slots_ok(tokens, k, 1) && dim >= 1 && rows >= 0 && rows <= (1 << 30) && ld0 >= dim && ld1 >= dim;
+}
+int elem_bytes(int dtype) { return dtype == BLS_F32 ? 4 : 2; }
+
+}  // namespace
+
+extern "C" {
+
+bls_status_t bls_moe_bytes(int64_t tokens, int k, int n_experts, size_t *bytes)
+{
+    if (!bytes || !slots_ok(tokens, k, n_experts)) return BLS_EINVAL;
+    *bytes = 0;
+    return BLS_OK;
+}
+
+bls_status_t bls_moe_route(const int32_t *expert, int64_t tokens, int k, int n_experts, int32_t *order, int32_t *place,
+                           int32_t *offsets, void *workspace, size_t bytes, void *cuda_stream)
+{
+    size_t need = 0;
+    if (bls_moe_bytes(tokens, k, n_experts, &need) != BLS_OK || !offsets || (tokens && (!expert || !order || !place))) return BLS_EINVAL;
+    if (bytes < need) return BLS_ENOSPC;
+    (void)workspace;
+    const size_t smem = sizeof(int) * ROUTE_WARPS * n_experts;
+    if (cudaFuncSetAttribute(bls_moe_route_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return BLS_ECUDA;
+    return launch_serialised_smem(bls_moe_route_kernel, dim3(1), dim3(ROUTE_THREADS), smem, (cudaStream_t)cuda_stream, expert,
+                                  (int)(tokens * k), n_experts, order, place, offsets) == cudaSuccess ? BLS_OK : BLS_ECUDA;
+}
+
+bls_status_t bls_moe_dispatch(const void *x, int64_t ldx, int dtype, const int32_t *place, const int32_t *offsets,
+                              int n_experts, int64_t tokens, int k, int dim, void *y, int64_t ldy, int64_t rows,
+                              void *cuda_stream)
+{
+    if (!move_ok(dtype, tokens, k, dim, rows, ldx, ldy) || n_experts < 1 || n_experts > MOE_MAX_EXPERTS || !offsets ||
+        (tokens && (!x || !place)) || (rows && !y))
+        return BLS_EINVAL;
+    if (rows == 0) return BLS_OK;
+    MoveArgs m = {};
+    m.a = x; m.lda = ldx; m.o = y; m.ldo = ldy; m.place = place; m.total = offsets + n_experts;
+    m.tokens = tokens; m.rows = rows; m.k = k;
+    const int eb = elem_bytes(dtype);
+    return launch_move(MOVE_DISPATCH, m, dtype, dim, whole_pieces(x, ldx, dim, eb) && whole_pieces(y, ldy, dim, eb), (cudaStream_t)cuda_stream);
+}
+
+bls_status_t bls_moe_combine(const void *y, int64_t ldy, int64_t rows, int dtype, const int32_t *place, const float *w,
+                             int64_t tokens, int k, int dim, void *out, int64_t ldo, void *cuda_stream)
+{
+    if (!move_ok(dtype, tokens, k, dim, rows, ldy, ldo) || (tokens && (!place || !out)) || (rows && !y)) return BLS_EINVAL;
+    if (tokens == 0) return BLS_OK;
+    MoveArgs m = {};
+    m.a = y; m.lda = ldy; m.o = out; m.ldo = ldo; m.place = place; m.w = w;
+    m.tokens = tokens; m.rows = rows; m.k = k;
+    const int eb = elem_bytes(dtype);
+    return launch_move(MOVE_COMBINE, m, dtype, dim, whole_pieces(y, ldy, dim, eb) && whole_pieces(out, ldo, dim, eb), (cudaStream_t)cuda_stream);
+}
+
+bls_status_t bls_moe_combine_grad(const void *dout, int64_t ldd, const void *y, int64_t ldy, int64_t rows, int dtype,
+                                  const int32_t *place, const int32_t *offsets, int n_experts, const float *w,
+                                  int64_t tokens, int k, int dim, void *dy, int64_t lddy, float *dw, void *cuda_stream)
+{
+    if (!move_ok(dtype, tokens, k, dim, rows, ldd, lddy) || n_experts < 1 || n_experts > MOE_MAX_EXPERTS || !offsets ||
+        (tokens && (!dout || !place)) || (rows && !dy) || (dw && rows && (!y || ldy < dim)))
+        return BLS_EINVAL;
+    if (rows == 0 && !(dw && tokens)) return BLS_OK;
+    MoveArgs m = {};
+    m.a = dout; m.lda = ldd; m.b = y; m.ldb = ldy; m.o = dy; m.ldo = lddy; m.place = place; m.total = offsets + n_experts;
+    m.w = w; m.dw = dw; m.tokens = tokens; m.rows = rows; m.k = k;
+    const int eb = elem_bytes(dtype);
+    const bool whole = whole_pieces(dout, ldd, dim, eb) && whole_pieces(dy, lddy, dim, eb) && (!dw || whole_pieces(y, ldy, dim, eb));
+    return launch_move(MOVE_GRAD, m, dtype, dim, whole, (cudaStream_t)cuda_stream);
+}
+
+}  // extern "C"
