@@ -419,7 +419,8 @@ bls_status_t bls_moe_combine_grad(const void *dout, int64_t ldd, const void *y, 
  *                      z = clamp(rint(-lo / s), 0, 15), q = clamp(rint(w / s) + z, 0, 15).  s = 0 gives
  *                      q = z; a NaN or an infinity makes its whole group NaN.  Quotients are fp32.
  *   bls_w4_dequantize  the weights (q - z) * s in fp32, rounded once to dtype
- *   bls_w4_bytes       workspace of bls_w4_linear (256-byte aligned; may be 0)
+ *   bls_w4_bytes       workspace of bls_w4_linear for these x, ldx and rows (256-byte aligned; may be 0:
+ *                      it is needed when rows of x do not start at 16-byte boundaries)
  *   bls_w4_linear      y[r][n] = act(bias[e][n] + sum over groups of s * sum of (q - z) * x[r][..]), e = the
  *                      matrix of row r: rows offsets[e] .. offsets[e + 1] - 1 (int32 [E + 1], as bls_moe_route
  *                      gives them; NULL with E = 1: all rows).  Rows from offsets[E] on are set to 0.
@@ -434,7 +435,7 @@ bls_status_t bls_w4_quantize(const void *w, int dtype, int64_t ldw, int E, int N
                              uint8_t *zero, void *cuda_stream);
 bls_status_t bls_w4_dequantize(const uint8_t *q, const void *scale, const uint8_t *zero, int E, int N, int K, int group,
                                void *w, int dtype, int64_t ldw, void *cuda_stream);
-bls_status_t bls_w4_bytes(int E, int N, int K, int64_t rows, size_t *bytes /*host*/);
+bls_status_t bls_w4_bytes(int E, int N, int K, const void *x, int64_t ldx, int64_t rows, size_t *bytes /*host*/);
 bls_status_t bls_w4_linear(const uint8_t *q, const void *scale, const uint8_t *zero, int E, int N, int K, int group,
                            const void *x, int x_dtype, int64_t ldx, int64_t rows, const int32_t *offsets,
                            const float *bias, int act, void *y, int y_dtype, int64_t ldy, void *workspace, size_t bytes,

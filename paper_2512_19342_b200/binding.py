@@ -73,7 +73,7 @@ def lib():
         _lib.bls_w4_sizes.argtypes = [i, i, i, i, p, p]
         _lib.bls_w4_quantize.argtypes = [p, i, l, i, i, i, i, p, p, p, p]
         _lib.bls_w4_dequantize.argtypes = [p, p, p, i, i, i, i, p, i, l, p]
-        _lib.bls_w4_bytes.argtypes = [i, i, i, l, p]
+        _lib.bls_w4_bytes.argtypes = [i, i, i, p, l, l, p]
         _lib.bls_w4_linear.argtypes = [p, p, p, i, i, i, i, p, i, l, l, p, p, i, p, i, l, p, C.c_size_t, p, p]
     return _lib
 
@@ -642,7 +642,7 @@ def bls_w4_linear(w4: W4, x: torch.Tensor, y: torch.Tensor, offsets: Optional[to
     _need(x.dtype != torch.float32, "x: expected bf16 or f16")
     _need(offsets is not None or w4.E == 1, "offsets are needed with more than one matrix")
     nbytes = C.c_size_t(0)
-    _check(lib().bls_w4_bytes(w4.E, w4.N, w4.K, rows, C.byref(nbytes)), "bls_w4_bytes")
+    _check(lib().bls_w4_bytes(w4.E, w4.N, w4.K, x.data_ptr(), _pitch(x), rows, C.byref(nbytes)), "bls_w4_bytes")
     ws = _scratch(nbytes.value, stream, x) if nbytes.value else None
     _check(_lib.bls_w4_linear(*w4._ptrs, x.data_ptr(), _DTYPE[x.dtype], _pitch(x), rows,
                               _flat(offsets, "offsets", (w4.E + 1,), torch.int32), _flat(bias, "bias", (w4.E, w4.N), torch.float32),

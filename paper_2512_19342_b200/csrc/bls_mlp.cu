@@ -13,14 +13,13 @@
 //
 // Every wait is bounded by the clock; a wait that gives up latches BLS_ST_ETIMEOUT in the
 // handle's status word, the roles wind down, and tensor memory is always released.
-#include <cuda.h>
-#include <cudaTypedefs.h>
 #include <cuda_bf16.h>
 #include <stdlib.h>
 #include <string.h>
 #include <new>
 #include <vector>
 #include "bls_internal.h"
+#include "bls_tc.cuh"
 
 namespace {
 
@@ -29,91 +28,11 @@ constexpr int MLP_BK = 64;           // K per stage: 64 bf16 = 128 bytes = one s
 constexpr int MLP_STAGES = 3;          // 3 x 32 KiB of tiles at BN = 128: two CTAs per SM, one computes while the other stores
 constexpr int MLP_THREADS = 192;     // warp 0: TMA, warp 1: MMA + TMEM allocation, warps 2-5: epilogue
 
-__device__ __forceinline__ unsigned long long mlp_clock()
-{
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-__device__ __forceinline__ unsigned s_addr(const void *p) { return (unsigned)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mb_init(unsigned bar, unsigned count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mb_expect_tx(unsigned bar, unsigned bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-// Bounded wait for the phase with the given parity: false (and the status bit) after two seconds.
-__device__ __forceinline__ bool mb_wait(unsigned bar, unsigned parity, int *status)
-{
-    unsigned tries = 0;
-    unsigned long long t0 = 0;
-    for (;;) {
-        unsigned ok;
-        asm volatile("{\n\t.reg .pred p;\n\t"
-                     "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-                     "selp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-        if (ok) return true;
-        if ((++tries & 255u) == 0) {
-            const unsigned long long now = mlp_clock();
-            if (t0 == 0) t0 = now;
-            else if (now - t0 > 2000000000ull) { atomicOr(status, BLS_ST_ETIMEOUT); return false; }
-        }
-    }
-}
-__device__ __forceinline__ void tma_load_2d(unsigned dst, const CUtensorMap *map, unsigned bar, int x, int y)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
-}
-// Shared-memory matrix descriptor of a K-major tile stored with the 128-byte swizzle:
-// rows of 128 bytes, groups of 8 rows 1024 bytes apart (stride byte offset), descriptor
-// version 1, layout type 2 (128-byte swizzle).  The leading byte offset is not used by
-// this layout.  `addr` is the byte address of the first row (a multiple of 1024) plus
-// the byte offset of the K slice inside the 128-byte row.
-__device__ __forceinline__ unsigned long long umma_desc(unsigned addr)
-{
-    unsigned long long d = 0;
-    d |= (unsigned long long)((addr >> 4) & 0x3FFFu);          // start address, 16-byte units
-    d |= (unsigned long long)1u << 16;                         // leading byte offset (unused), 16-byte units
-    d |= (unsigned long long)(1024u >> 4) << 32;               // stride byte offset: 8 rows x 128 bytes
-    d |= (unsigned long long)1u << 46;                         // descriptor version of this architecture
-    d |= (unsigned long long)2u << 61;                         // 128-byte swizzle
-    return d;
-}
 // Instruction descriptor: fp32 accumulator, bf16 A and B, both K-major, M = 128, N = n.
 __device__ __forceinline__ unsigned umma_idesc(int n)
 {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((unsigned)(n >> 3) << 17) | ((unsigned)(MLP_BM >> 4) << 24);
 }
-__device__ __forceinline__ void umma_f16(unsigned d_tmem, unsigned long long da, unsigned long long db, unsigned idesc, unsigned acc)
-{
-    asm volatile("{\n\t.reg .pred p;\n\t"
-                 "setp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d_tmem), "l"(da), "l"(db), "r"(idesc), "r"(acc) : "memory");
-}
-// The mbarrier gets one arrival once every MMA issued so far by this thread has completed.
-__device__ __forceinline__ void umma_commit(unsigned bar)
-{
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tmem_ld32(unsigned taddr, unsigned (&r)[32])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-                   "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-                 : "r"(taddr) : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-
 struct LinArgs {
     int M, N, K;
     const float *bias;      // [N]
@@ -325,34 +244,6 @@ __global__ void __launch_bounds__(64) bls_interact_kernel(const __nv_bfloat16 *x
     for (int c = D + npairs + threadIdx.x; c < ldr; c += blockDim.x) out[c] = __float2bfloat16_rn(0.f);
 }
 
-PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
-
-bool encode_ready()
-{
-    if (g_encode) return true;
-    void *fn = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess || !fn ||
-        qres != cudaDriverEntryPointSuccess)
-        return false;
-    g_encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
-    return true;
-}
-
-// Tensor map of a row-major bf16 matrix [rows][cols] with row pitch ld elements: boxes of 64 columns x box_rows rows,
-// 128-byte swizzle, zero fill outside the matrix.
-bool make_map(CUtensorMap *map, const void *base, long long rows, long long cols, long long ld, int box_rows)
-{
-    if (!encode_ready()) return false;
-    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-    cuuint32_t box[2] = {(cuuint32_t)MLP_BK, (cuuint32_t)box_rows};
-    cuuint32_t estr[2] = {1, 1};
-    return g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, estr,
-                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 int pick_bn(int N) { return N > 64 ? 128 : (N > 32 ? 64 : 32); }
 
 template <int BN>
@@ -423,10 +314,10 @@ bls_status_t bls_mlp_create(int n_layers, const int *dims, const void *const *we
         if (!weights[i] || !bias[i] || ((uintptr_t)weights[i] & 15)) { delete h; return BLS_EINVAL; }
         h->weights.push_back(weights[i]);
         h->bias.push_back(bias[i]);
-        if (!make_map(&h->map_w[i], weights[i], dims[i + 1], dims[i], dims[i], pick_bn(dims[i + 1]))) { delete h; return BLS_ECUDA; }
+        if (!tc_make_map(&h->map_w[i], weights[i], dims[i + 1], dims[i], dims[i], pick_bn(dims[i + 1]))) { delete h; return BLS_ECUDA; }
         if (i + 1 < n_layers) {
             h->hidden.push_back(ws + o);
-            if (!make_map(&h->map_h[i], ws + o, max_rows, dims[i + 1], dims[i + 1], MLP_BM)) { delete h; return BLS_ECUDA; }
+            if (!tc_make_map(&h->map_h[i], ws + o, max_rows, dims[i + 1], dims[i + 1], MLP_BM)) { delete h; return BLS_ECUDA; }
             o += ((size_t)max_rows * dims[i + 1] * 2 + 255) / 256 * 256;
         }
     }
@@ -444,7 +335,7 @@ bls_status_t bls_mlp_forward(bls_mlp_t *h, const void *x, int ldx, int rows, voi
         return BLS_EINVAL;
     cudaStream_t s = (cudaStream_t)cuda_stream;
     CUtensorMap map_x;
-    if (!make_map(&map_x, x, rows, h->dims[0], ldx, MLP_BM)) return BLS_ECUDA;
+    if (!tc_make_map(&map_x, x, rows, h->dims[0], ldx, MLP_BM)) return BLS_ECUDA;
     for (int i = 0; i < h->n_layers; i++) {
         const bool last = i + 1 == h->n_layers;
         LinArgs a;

@@ -8,6 +8,7 @@
 // only the unpacking.  The order of the inputs inside a product is free, so a lane
 // takes the inputs that one stored 16-byte piece holds, and reads the same 8 neighbouring x values per word.
 #include "bls_w4.cuh"
+#include "bls_w4_gemm.h"
 
 namespace {
 
@@ -222,6 +223,9 @@ bool w4_shape(int E, int N, int K, int group, W4Weights &w)
     return true;
 }
 
+// Which kernel: by the rows that a matrix gets on average.
+bool many_rows(const W4Weights &w, int64_t rows) { return rows > 32ll * w.E; }
+
 template <class T, int NT>
 cudaError_t launch_rows(const W4Args &a, cudaStream_t s)
 {
@@ -268,11 +272,11 @@ bls_status_t bls_w4_dequantize(const uint8_t *q, const void *scale, const uint8_
            cudaSuccess ? BLS_OK : BLS_ECUDA;
 }
 
-bls_status_t bls_w4_bytes(int E, int N, int K, int64_t rows, size_t *bytes)
+bls_status_t bls_w4_bytes(int E, int N, int K, const void *x, int64_t ldx, int64_t rows, size_t *bytes)
 {
     W4Weights d;
     if (!bytes || rows < 0 || rows > (1 << 30) || !w4_shape(E, N, K, 32, d)) return BLS_EINVAL;
-    *bytes = 0;
+    *bytes = many_rows(d, rows) ? w4_tiles_bytes(d, x, ldx, rows) : 0;
     return BLS_OK;
 }
 
@@ -283,17 +287,18 @@ bls_status_t bls_w4_linear(const uint8_t *q, const void *scale, const uint8_t *z
 {
     W4Args a = {};
     size_t need = 0;
-    if (!q || !scale || ((uintptr_t)q & 15) || !w4_shape(E, N, K, group, a.w) || bls_w4_bytes(E, N, K, rows, &need) != BLS_OK ||
+    if (!q || !scale || ((uintptr_t)q & 15) || !w4_shape(E, N, K, group, a.w) || bls_w4_bytes(E, N, K, x, ldx, rows, &need) != BLS_OK ||
         (x_dtype != BLS_BF16 && x_dtype != BLS_F16) || y_dtype < 0 || y_dtype > 2 || act < 0 || act > 2 || ldx < K || ldy < N ||
         (!offsets && E != 1) || (rows && (!x || !y)) || !status)
         return BLS_EINVAL;
     if (bytes < need) return BLS_ENOSPC;
-    (void)workspace;
+    if (need && (!workspace || ((uintptr_t)workspace & 255))) return BLS_EINVAL;
     if (rows == 0) return BLS_OK;
     a.w.q = q; a.w.scale = (const __nv_bfloat16 *)scale; a.w.zero = zero;
     a.x = x; a.ldx = ldx; a.rows = (int)rows; a.x_pieces = ((uintptr_t)x & 15) == 0 && ldx % 8 == 0;
     a.offsets = offsets; a.bias = bias; a.act = act; a.y = y; a.y_dtype = y_dtype; a.ldy = ldy; a.status = status;
-    cudaError_t r = x_dtype == BLS_BF16 ? launch_linear4<__nv_bfloat16>(a, (cudaStream_t)cuda_stream) : launch_linear4<__half>(a, (cudaStream_t)cuda_stream);
+    cudaError_t r = many_rows(a.w, rows) ? w4_tiles(a, x_dtype, workspace, (cudaStream_t)cuda_stream) :
+                    x_dtype == BLS_BF16 ? launch_linear4<__nv_bfloat16>(a, (cudaStream_t)cuda_stream) : launch_linear4<__half>(a, (cudaStream_t)cuda_stream);
     return r == cudaSuccess ? BLS_OK : BLS_ECUDA;
 }
 

@@ -550,7 +550,7 @@ def test_calls_refuse_bad_arguments():
     n = C.c_size_t(0)
     assert lib.bls_moe_bytes(-1, 2, 8, C.byref(n)) == bls.BLS_EINVAL
     assert lib.bls_moe_bytes(1 << 30, 2, 8, C.byref(n)) == bls.BLS_EINVAL
-    assert lib.bls_w4_bytes(1, 8, 0, 5, C.byref(n)) == bls.BLS_EINVAL
+    assert lib.bls_w4_bytes(1, 8, 0, None, 8, 5, C.byref(n)) == bls.BLS_EINVAL
     assert bls.bls_w4_sizes(2, 129, 130, 64) == (2 * 2 * 2 * 8192, 2 * 2 * 2 * 2 * 128)
     # a misaligned q and a missing status word are refused by the library itself
     p = t._ptrs
