@@ -372,7 +372,7 @@ bls_status_t bls_mlp_status(bls_mlp_t *handle, void *cuda_stream);
  * expert int32 [tokens][k]: the expert of every slot.  An ID outside [0, n_experts) names no expert
  * held here (a masked token, a dropped slot, an expert of another rank): that slot is left out.
  * tokens may be 0; tokens * k and rows at most 2^30; 1 <= k <= 1024, 1 <= n_experts <= 1024.
- *   bls_moe_bytes    workspace of bls_moe_route (256-byte aligned; may be 0)
+ *   bls_moe_bytes    workspace of bls_moe_route (256-byte aligned; 0 up to 4096 slots)
  *   bls_moe_route    stable sort of the kept slots by expert:
  *                    offsets int32 [n_experts + 1]  first sorted position of every expert, then the number of kept slots
  *                    order   int32 [tokens * k]     slot t * k + i at every sorted position, -1 past offsets[n_experts]
@@ -419,8 +419,8 @@ bls_status_t bls_moe_combine_grad(const void *dout, int64_t ldd, const void *y, 
  *                      z = clamp(rint(-lo / s), 0, 15), q = clamp(rint(w / s) + z, 0, 15).  s = 0 gives
  *                      q = z; a NaN or an infinity makes its whole group NaN.  Quotients are fp32.
  *   bls_w4_dequantize  the weights (q - z) * s in fp32, rounded once to dtype
- *   bls_w4_bytes       workspace of bls_w4_linear for these x, ldx and rows (256-byte aligned; may be 0:
- *                      it is needed when rows of x do not start at 16-byte boundaries)
+ *   bls_w4_bytes       workspace of bls_w4_linear for these x, ldx and rows (256-byte aligned; 0 up to
+ *                      32 rows, and when rows of x start at 16-byte boundaries)
  *   bls_w4_linear      y[r][n] = act(bias[e][n] + sum over groups of s * sum of (q - z) * x[r][..]), e = the
  *                      matrix of row r: rows offsets[e] .. offsets[e + 1] - 1 (int32 [E + 1], as bls_moe_route
  *                      gives them; NULL with E = 1: all rows).  Rows from offsets[E] on are set to 0.

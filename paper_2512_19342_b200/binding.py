@@ -7,6 +7,7 @@ no CPU fallback: if the shared library is missing the first call raises.
 from __future__ import annotations
 
 import collections
+import contextlib
 import ctypes as C
 import os
 from typing import Optional, Sequence
@@ -456,9 +457,16 @@ def bls_interact(x: torch.Tensor, pooled: torch.Tensor, r: torch.Tensor, stream:
 
 # ---- the expert stage ----
 
+# These calls are as short as a token's worth of work on the GPU, so the checks are single expressions and sizes
+# that need no workspace do not ask for one.
+
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
+    lambda device: torch.cuda.current_stream(device).cuda_stream
+
+
 def _on(stream: Optional[torch.cuda.Stream], like: torch.Tensor) -> int:
     """Handle of the stream that a call on `like` is enqueued on."""
-    return stream.cuda_stream if stream is not None else torch.cuda.current_stream(like.device).cuda_stream
+    return _raw_stream(like.get_device()) if stream is None else stream.cuda_stream
 
 
 def _scratch(n: int, stream: Optional[torch.cuda.Stream], like: torch.Tensor) -> torch.Tensor:
@@ -474,99 +482,118 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
-def _rows(t: torch.Tensor, name: str, shape, dtype: Optional[torch.dtype] = None):
-    """A matrix whose rows are contiguous (any row pitch), of one type, on a GPU."""
-    _need(t.is_cuda and t.dim() == 2 and tuple(t.shape) == tuple(shape) and (t.shape[1] < 2 or t.stride(1) == 1) and
-          (t.shape[0] < 2 or t.stride(0) >= t.shape[1]) and (t.dtype == dtype if dtype else t.dtype in _DTYPE),
-          f"{name}: expected a CUDA matrix {tuple(shape)}{' of ' + str(dtype) if dtype else ''} with contiguous rows")
-
-
-def _pitch(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
-
-
-def _flat(t: Optional[torch.Tensor], name: str, shape, dtype: torch.dtype):
-    """A contiguous tensor of one shape and type on a GPU; its address (None stays None)."""
+def _flat(t: Optional[torch.Tensor], name: str, shape: tuple, dtype: torch.dtype):
+    """Address of a contiguous tensor of one shape and type on a GPU (None stays None)."""
     if t is None:
         return None
-    _need(t.is_cuda and t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
-          f"{name}: expected a contiguous CUDA tensor {tuple(shape)} of {dtype}")
-    return t.data_ptr()
+    if t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: expected a contiguous CUDA tensor {shape} of {dtype}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+
+
+def _rows(t: torch.Tensor, name: str, shape: tuple, dtype: torch.dtype):
+    """(address, row pitch) of a matrix of one type on a GPU whose rows are contiguous, at any pitch."""
+    if t.is_cuda and t.dtype is dtype and t.shape == shape:
+        ld, step = t.stride()
+        if shape[0] < 2:
+            ld = max(shape[1], 1)
+        if (step == 1 or shape[1] < 2) and ld >= shape[1]:
+            return t.data_ptr(), max(ld, 1)
+    raise ValueError(f"{name}: expected a CUDA matrix {shape} of {dtype} with contiguous rows, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}, on {t.device}")
+
+
+def _two(t: torch.Tensor, name: str) -> tuple:
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected a matrix, got {tuple(t.shape)}")
+    return t.shape
+
+
+def _dt(t: torch.Tensor, name: str) -> int:
+    d = _DTYPE.get(t.dtype)
+    if d is None:
+        raise ValueError(f"{name}: expected fp32, bf16 or f16, got {t.dtype}")
+    return d
+
+
+_I32, _F32 = torch.int32, torch.float32
 
 
 def bls_moe_route(expert: torch.Tensor, n_experts: int, order: torch.Tensor, place: torch.Tensor, offsets: torch.Tensor,
                   stream: Optional[torch.cuda.Stream] = None) -> None:
     """Stable sort of the slots expert int32 [n][k] by expert; IDs outside [0, n_experts) leave their slot out.
     order int32 [n*k], place int32 [n][k], offsets int32 [n_experts+1] are written."""
-    _need(expert.dim() == 2, "expert: expected [tokens][k]")
-    n, k = expert.shape
-    i32 = torch.int32
-    args = (_flat(expert, "expert", (n, k), i32), n, k, n_experts, _flat(order, "order", (n * k,), i32),
-            _flat(place, "place", (n, k), i32), _flat(offsets, "offsets", (n_experts + 1,), i32))
-    nbytes = C.c_size_t(0)
-    _check(lib().bls_moe_bytes(n, k, n_experts, C.byref(nbytes)), "bls_moe_bytes")
-    ws = _scratch(nbytes.value, stream, expert) if nbytes.value else None
-    _check(_lib.bls_moe_route(*args, ws.data_ptr() if ws is not None else None, nbytes.value, _on(stream, expert)), "bls_moe_route")
+    n, k = _two(expert, "expert")
+    args = (_flat(expert, "expert", (n, k), _I32), n, k, n_experts, _flat(order, "order", (n * k,), _I32),
+            _flat(place, "place", (n, k), _I32), _flat(offsets, "offsets", (n_experts + 1,), _I32))
+    l = lib()
+    ws, nbytes = None, 0
+    if n * k > 4096:                         # fewer slots never need a workspace
+        size = C.c_size_t(0)
+        _check(l.bls_moe_bytes(n, k, n_experts, C.byref(size)), "bls_moe_bytes")
+        nbytes = size.value
+        ws = _scratch(nbytes, stream, expert)
+    code = l.bls_moe_route(*args, ws.data_ptr() if nbytes else None, nbytes, _on(stream, expert))
+    if code:
+        raise BlsError(code, "bls_moe_route")
 
 
 def bls_moe_dispatch(x: torch.Tensor, place: torch.Tensor, offsets: torch.Tensor, y: torch.Tensor,
                      stream: Optional[torch.cuda.Stream] = None) -> None:
     """y[place[t][i]] = x[t]; the rows of y from offsets[-1] on become 0.  x [n][D], y [rows][D] of one type."""
-    _need(place.dim() == 2 and y.dim() == 2 and x.dim() == 2, "x, y and place are matrices")
-    n, k = place.shape
-    D = x.shape[1]
-    _rows(x, "x", (n, D))
-    _rows(y, "y", (y.shape[0], D), x.dtype)
-    _check(lib().bls_moe_dispatch(x.data_ptr(), _pitch(x), _DTYPE[x.dtype], _flat(place, "place", (n, k), torch.int32),
-                                  _flat(offsets, "offsets", (offsets.numel(),), torch.int32), offsets.numel() - 1, n, k, D,
-                                  y.data_ptr(), _pitch(y), y.shape[0], _on(stream, x)), "bls_moe_dispatch")
+    n, k = _two(place, "place")
+    D, R, dt = _two(x, "x")[1], _two(y, "y")[0], x.dtype
+    px, ldx = _rows(x, "x", (n, D), dt)
+    py, ldy = _rows(y, "y", (R, D), dt)
+    e = offsets.numel()
+    code = lib().bls_moe_dispatch(px, ldx, _dt(x, "x"), _flat(place, "place", (n, k), _I32), _flat(offsets, "offsets", (e,), _I32), e - 1,
+                                  n, k, D, py, ldy, R, _on(stream, x))
+    if code:
+        raise BlsError(code, "bls_moe_dispatch")
 
 
 def bls_moe_combine(y: torch.Tensor, place: torch.Tensor, w: Optional[torch.Tensor], out: torch.Tensor,
                     stream: Optional[torch.cuda.Stream] = None) -> None:
     """out[t] = sum over i of w[t][i] * y[place[t][i]] (w fp32 [n][k] or None: all 1).  y [rows][D], out [n][D] of one type."""
-    _need(place.dim() == 2 and y.dim() == 2 and out.dim() == 2, "y, out and place are matrices")
-    n, k = place.shape
-    D = out.shape[1]
-    _rows(out, "out", (n, D))
-    _rows(y, "y", (y.shape[0], D), out.dtype)
-    _check(lib().bls_moe_combine(y.data_ptr(), _pitch(y), y.shape[0], _DTYPE[y.dtype], _flat(place, "place", (n, k), torch.int32),
-                                 _flat(w, "w", (n, k), torch.float32), n, k, D, out.data_ptr(), _pitch(out), _on(stream, y)),
-           "bls_moe_combine")
+    n, k = _two(place, "place")
+    D, R, dt = _two(out, "out")[1], _two(y, "y")[0], y.dtype
+    po, ldo = _rows(out, "out", (n, D), dt)
+    py, ldy = _rows(y, "y", (R, D), dt)
+    code = lib().bls_moe_combine(py, ldy, R, _dt(y, "y"), _flat(place, "place", (n, k), _I32), _flat(w, "w", (n, k), _F32),
+                                 n, k, D, po, ldo, _on(stream, y))
+    if code:
+        raise BlsError(code, "bls_moe_combine")
 
 
 def bls_moe_combine_grad(dout: torch.Tensor, y: Optional[torch.Tensor], place: torch.Tensor, offsets: torch.Tensor,
                          w: Optional[torch.Tensor], dy: torch.Tensor, dw: Optional[torch.Tensor] = None,
                          stream: Optional[torch.cuda.Stream] = None) -> None:
     """Gradients of bls_moe_combine: dy[place[t][i]] = w[t][i] * dout[t] and, if wanted, dw[t][i] = <dout[t], y[place[t][i]]>."""
-    _need(place.dim() == 2 and dout.dim() == 2 and dy.dim() == 2, "dout, dy and place are matrices")
-    n, k = place.shape
-    D, rows = dout.shape[1], dy.shape[0]
-    _rows(dout, "dout", (n, D))
-    _rows(dy, "dy", (rows, D), dout.dtype)
-    _need(dw is None or y is not None, "dw needs y")
+    n, k = _two(place, "place")
+    D, R, dt = _two(dout, "dout")[1], _two(dy, "dy")[0], dout.dtype
+    pd, ldd = _rows(dout, "dout", (n, D), dt)
+    pg, ldg = _rows(dy, "dy", (R, D), dt)
+    py, ldy = None, D
     if dw is not None:
-        _rows(y, "y", (rows, D), dout.dtype)
-    else:
-        y = None
-    _check(lib().bls_moe_combine_grad(dout.data_ptr(), _pitch(dout), y.data_ptr() if y is not None else None,
-                                      _pitch(y) if y is not None else D, rows, _DTYPE[dout.dtype],
-                                      _flat(place, "place", (n, k), torch.int32),
-                                      _flat(offsets, "offsets", (offsets.numel(),), torch.int32), offsets.numel() - 1,
-                                      _flat(w, "w", (n, k), torch.float32), n, k, D, dy.data_ptr(), _pitch(dy),
-                                      _flat(dw, "dw", (n, k), torch.float32), _on(stream, dout)), "bls_moe_combine_grad")
+        _need(y is not None, "dw needs y")
+        py, ldy = _rows(y, "y", (R, D), dt)
+    e = offsets.numel()
+    code = lib().bls_moe_combine_grad(pd, ldd, py, ldy, R, _dt(dout, "dout"), _flat(place, "place", (n, k), _I32),
+                                      _flat(offsets, "offsets", (e,), _I32), e - 1, _flat(w, "w", (n, k), _F32), n, k, D, pg, ldg,
+                                      _flat(dw, "dw", (n, k), _F32), _on(stream, dout))
+    if code:
+        raise BlsError(code, "bls_moe_combine_grad")
 
 
 class W4:
     """E matrices [N][K] in 4 bits with group scales: the three tensors of the storage format (include/bls.h)."""
-    __slots__ = ("q", "scale", "zero", "E", "N", "K", "group", "_ptrs")
+    __slots__ = ("q", "scale", "zero", "E", "N", "K", "group", "_args")
 
     def __init__(self, q: torch.Tensor, scale: torch.Tensor, zero: Optional[torch.Tensor], N: int, K: int, group: int):
-        nt, kt = (N + 127) // 128, (K + 127) // 128
-        _need(group in (32, 64, 128) and N >= 1 and K >= 1 and q.dim() == 5, "W4: bad sizes")
-        E = q.shape[0]
+        if group not in (32, 64, 128) or N < 1 or K < 1 or q.dim() != 5:
+            raise ValueError("W4: bad sizes")
+        nt, kt, E = (N + 127) // 128, (K + 127) // 128, q.shape[0]
         shape = (E, kt * 128 // group, nt * 128)
-        self._ptrs = (_flat(q, "q", (E, nt, kt, 128, 64), torch.uint8), _flat(scale, "scale", shape, torch.bfloat16),
+        self._args = (_flat(q, "q", (E, nt, kt, 128, 64), torch.uint8), _flat(scale, "scale", shape, torch.bfloat16),
                       _flat(zero, "zero", shape, torch.uint8), E, N, K, group)
         self.q, self.scale, self.zero, self.E, self.N, self.K, self.group = q, scale, zero, E, N, K, group
 
@@ -592,14 +619,12 @@ def bls_w4_quantize(w: torch.Tensor, group: int = 128, symmetric: bool = True, s
     E, N, K, ld = _matrices(w, "w")
     _need(group in (32, 64, 128), "group: 32, 64 or 128")
     nt, kt = (N + 127) // 128, (K + 127) // 128
-    ns = E * kt * (128 // group) * nt * 128
-    nq = E * nt * kt * 8192
-    buf = _scratch(nq + ns * (2 if symmetric else 3), stream, w)           # one allocation: q, scale, zero
     shape = (E, kt * 128 // group, nt * 128)
-    t = W4(buf[:nq].view(E, nt, kt, 128, 64), buf[nq:nq + 2 * ns].view(torch.bfloat16).view(shape),
-           None if symmetric else buf[nq + 2 * ns:].view(shape), N, K, group)
-    _check(lib().bls_w4_quantize(w.data_ptr(), _DTYPE[w.dtype], ld, E, N, K, group, t._ptrs[0], t._ptrs[1], t._ptrs[2],
-                                 _on(stream, w)), "bls_w4_quantize")
+    with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():      # memory of the call's own stream
+        q, scale = w.new_empty((E, nt, kt, 128, 64), dtype=torch.uint8), w.new_empty(shape, dtype=torch.bfloat16)
+        zero = None if symmetric else w.new_empty(shape, dtype=torch.uint8)
+    t = W4(q, scale, zero, N, K, group)
+    _check(lib().bls_w4_quantize(w.data_ptr(), _DTYPE[w.dtype], ld, E, N, K, group, *t._args[:3], _on(stream, w)), "bls_w4_quantize")
     return t
 
 
@@ -607,27 +632,27 @@ def bls_w4_dequantize(w4: W4, w: torch.Tensor, stream: Optional[torch.cuda.Strea
     """w [E][N][K] (or [N][K] with E = 1) = (q - z) * s, rounded once to w's type."""
     E, N, K, ld = _matrices(w, "w")
     _need((E, N, K) == (w4.E, w4.N, w4.K), f"w: expected {(w4.E, w4.N, w4.K)}")
-    _check(lib().bls_w4_dequantize(*w4._ptrs, w.data_ptr(), _DTYPE[w.dtype], ld, _on(stream, w)), "bls_w4_dequantize")
+    _check(lib().bls_w4_dequantize(*w4._args, w.data_ptr(), _DTYPE[w.dtype], ld, _on(stream, w)), "bls_w4_dequantize")
 
 
-_w4_status_word = {}                         # device -> int32 [1], zeroed once: bounded waits that gave up are latched here
+_w4_status_word = {}                         # device number -> (int32 [1], its address), zeroed once: waits that gave up are latched here
 
 
-def _status_word(device: torch.device) -> torch.Tensor:
+def _status_word(device: int):
     t = _w4_status_word.get(device)
     if t is None:
-        t = _w4_status_word[device] = torch.zeros(1, dtype=torch.int32, device=device)
+        word = torch.zeros(1, dtype=_I32, device=torch.device("cuda", device))
         torch.cuda.synchronize(device)       # once: calls on any stream may use it from here on
+        t = _w4_status_word[device] = (word, word.data_ptr())
     return t
 
 
-def bls_w4_status(device="cuda") -> int:
+def bls_w4_status(device=None) -> int:
     """Synchronises the device; BLS_ETIMEOUT if a bounded wait inside a 4-bit product gave up."""
-    device = torch.device(device)
-    if device.index is None:
-        device = torch.device("cuda", torch.cuda.current_device())
-    torch.cuda.synchronize(device)
-    return BLS_ETIMEOUT if int(_status_word(device).item()) & 8 else BLS_OK
+    index = torch.device("cuda" if device is None else device).index
+    index = torch.cuda.current_device() if index is None else index
+    torch.cuda.synchronize(index)
+    return BLS_ETIMEOUT if int(_status_word(index)[0].item()) & 8 else BLS_OK
 
 
 def bls_w4_linear(w4: W4, x: torch.Tensor, y: torch.Tensor, offsets: Optional[torch.Tensor] = None,
@@ -635,16 +660,21 @@ def bls_w4_linear(w4: W4, x: torch.Tensor, y: torch.Tensor, offsets: Optional[to
     """y = act(x W^T + bias), row by row with the matrix that offsets int32 [E+1] gives it (None with E = 1); rows from
     offsets[-1] on become 0.  x [rows][K] bf16 or f16, y [rows][N] bf16, f16 or fp32, bias fp32 [E][N];
     act 0 none, 1 ReLU, 2 logistic function."""
-    _need(x.dim() == 2, "x is a matrix")
-    rows = x.shape[0]
-    _rows(x, "x", (rows, w4.K))
-    _rows(y, "y", (rows, w4.N))
-    _need(x.dtype != torch.float32, "x: expected bf16 or f16")
-    _need(offsets is not None or w4.E == 1, "offsets are needed with more than one matrix")
-    nbytes = C.c_size_t(0)
-    _check(lib().bls_w4_bytes(w4.E, w4.N, w4.K, x.data_ptr(), _pitch(x), rows, C.byref(nbytes)), "bls_w4_bytes")
-    ws = _scratch(nbytes.value, stream, x) if nbytes.value else None
-    _check(_lib.bls_w4_linear(*w4._ptrs, x.data_ptr(), _DTYPE[x.dtype], _pitch(x), rows,
-                              _flat(offsets, "offsets", (w4.E + 1,), torch.int32), _flat(bias, "bias", (w4.E, w4.N), torch.float32),
-                              act, y.data_ptr(), _DTYPE[y.dtype], _pitch(y), ws.data_ptr() if ws is not None else None, nbytes.value,
-                              _status_word(x.device).data_ptr(), _on(stream, x)), "bls_w4_linear")
+    E, N, K = w4.E, w4.N, w4.K
+    rows = _two(x, "x")[0]
+    if x.dtype is _F32 or (offsets is None and E != 1):
+        raise ValueError("x: expected bf16 or f16" if x.dtype is _F32 else "offsets are needed with more than one matrix")
+    px, ldx = _rows(x, "x", (rows, K), x.dtype)
+    py, ldy = _rows(y, "y", (rows, N), y.dtype)
+    l = lib()
+    ws, nbytes = None, 0
+    if rows > 32:                            # fewer rows never need a workspace
+        size = C.c_size_t(0)
+        _check(l.bls_w4_bytes(E, N, K, px, ldx, rows, C.byref(size)), "bls_w4_bytes")
+        nbytes = size.value
+        if nbytes:
+            ws = _scratch(nbytes, stream, x)
+    code = l.bls_w4_linear(*w4._args, px, _dt(x, "x"), ldx, rows, _flat(offsets, "offsets", (E + 1,), _I32), _flat(bias, "bias", (E, N), _F32),
+                           act, py, _dt(y, "y"), ldy, ws.data_ptr() if nbytes else None, nbytes, _status_word(x.get_device())[1], _on(stream, x))
+    if code:
+        raise BlsError(code, "bls_w4_linear")

@@ -4,7 +4,9 @@
 // Routing is a stable counting sort.  A tile of consecutive slots is counted per warp, an
 // exclusive scan over (expert, tile, warp) gives every warp its first position for every
 // expert, and inside a warp the position of a slot is the number of lower lanes with the same
-// expert (match.any).  Positions depend on scans only: the result is the unique stable sort, the
+// expert (match.any).  Up to ROUTE_ONE slots one block does it all; more take a kernel that counts
+// the tiles and one in which every block adds up the counts before its own (tiles x E integers
+// from L2) and sorts its tile.  Positions depend on scans only: the result is the unique stable sort, the
 // same in every run.
 //
 // The moves are bound by memory: every row is read and written once, sums are fp32.
@@ -17,6 +19,7 @@ namespace {
 
 constexpr int ROUTE_THREADS = 1024;
 constexpr int ROUTE_WARPS = ROUTE_THREADS / 32;
+constexpr int ROUTE_ONE = 4096;              // slots that one block sorts alone
 constexpr int MOE_MAX_EXPERTS = 1024;
 constexpr int MOVE_THREADS = 256;
 
@@ -44,17 +47,39 @@ __device__ __forceinline__ int block_scan(int v, int *scratch)
     return v + (warp ? scratch[warp - 1] : 0);
 }
 
-// One block sorts all slots.  hist [ROUTE_WARPS][E]: counts, then first positions, of every warp.
-__global__ void __launch_bounds__(ROUTE_THREADS) bls_moe_route_kernel(const int *expert, int n, int E, int *order, int *place, int *offsets)
+// Counts of a tile's experts: row blockIdx.x of count [tiles][E].
+__global__ void __launch_bounds__(ROUTE_THREADS) bls_moe_count_kernel(const int *expert, int n, int E, int tile, int *count)
+{
+    stream_order_enter();
+    extern __shared__ int hist[];
+    for (int e = threadIdx.x; e < E; e += ROUTE_THREADS) hist[e] = 0;
+    __syncthreads();
+    const int lo = blockIdx.x * tile, hi = min(lo + tile, n);
+    for (int i = lo + threadIdx.x; i < hi; i += ROUTE_THREADS) {
+        const int e = expert[i];
+        if ((unsigned)e < (unsigned)E) atomicAdd(&hist[e], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += ROUTE_THREADS) count[(size_t)blockIdx.x * E + e] = hist[e];
+}
+
+// Sorts tile blockIdx.x of the slots.  TILED: count holds the counts of all tiles, and the block adds up
+// what lies before it; otherwise there is one block, which counts for itself.
+// hist [ROUTE_WARPS][E]: counts, then first positions, of every warp; TILED: two more rows.
+template <bool TILED>
+__global__ void __launch_bounds__(ROUTE_THREADS) bls_moe_route_kernel(const int *expert, int n, int E, int tile, const int *count,
+                                                                      int *order, int *place, int *offsets)
 {
     stream_order_enter();
     extern __shared__ int hist[];
     __shared__ int scratch[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int i = threadIdx.x; i < ROUTE_WARPS * E; i += ROUTE_THREADS) hist[i] = 0;
+    const int t0 = TILED ? blockIdx.x * tile : 0, t1 = min(t0 + tile, n);
+    int *all = hist + ROUTE_WARPS * E, *before = all + E;
+    for (int i = threadIdx.x; i < (ROUTE_WARPS + (TILED ? 2 : 0)) * E; i += ROUTE_THREADS) hist[i] = 0;
     __syncthreads();
-    const int per = ((n + ROUTE_WARPS - 1) / ROUTE_WARPS + 31) & ~31;         // consecutive slots of a warp
-    const int lo = min((long long)warp * per, (long long)n), hi = min((long long)lo + per, (long long)n);
+    const int per = ((t1 - t0 + ROUTE_WARPS - 1) / ROUTE_WARPS + 31) & ~31;   // consecutive slots of a warp
+    const int lo = min(t0 + warp * per, t1), hi = min(lo + per, t1);
     int *mine = hist + warp * E;
     for (int i = lo; i < hi; i += 32) {
         const int e = i + lane < hi ? expert[i + lane] : -1;
@@ -63,15 +88,36 @@ __global__ void __launch_bounds__(ROUTE_THREADS) bls_moe_route_kernel(const int 
         if (kept && lane == __ffs(same) - 1) mine[e] += __popc(same);
         __syncwarp();
     }
+    if (TILED) {
+        // every thread adds up one expert over a part of the tiles
+        const int parts = E < ROUTE_THREADS ? ROUTE_THREADS / E : 1;
+        const int e = threadIdx.x % E, part = threadIdx.x / E;
+        if (part < parts) {
+            int sum = 0, low = 0;
+            #pragma unroll 8
+            for (int t = part; t < (int)gridDim.x; t += parts) {
+                const int c = count[(size_t)t * E + e];
+                sum += c;
+                low += t < (int)blockIdx.x ? c : 0;
+            }
+            atomicAdd(&all[e], sum);
+            atomicAdd(&before[e], low);
+        }
+    }
     __syncthreads();
     int total = 0;
-    if (threadIdx.x < E)
-        for (int w = 0; w < ROUTE_WARPS; w++) total += hist[w * E + threadIdx.x];
+    if (threadIdx.x < E) {
+        if (TILED) total = all[threadIdx.x];
+        else for (int w = 0; w < ROUTE_WARPS; w++) total += hist[w * E + threadIdx.x];
+    }
     const int incl = block_scan(total, scratch);
     if (threadIdx.x < E) {
         int at = incl - total;
-        offsets[threadIdx.x] = at;
-        if (threadIdx.x == E - 1) offsets[E] = incl;
+        if (blockIdx.x == 0) {
+            offsets[threadIdx.x] = at;
+            if (threadIdx.x == E - 1) offsets[E] = incl;
+        }
+        if (TILED) at += before[threadIdx.x];
         for (int w = 0; w < ROUTE_WARPS; w++) {
             const int c = hist[w * E + threadIdx.x];
             hist[w * E + threadIdx.x] = at;
@@ -95,8 +141,17 @@ __global__ void __launch_bounds__(ROUTE_THREADS) bls_moe_route_kernel(const int 
         }
         __syncwarp();
     }
-    // scratch[31] still holds the number of kept slots
-    for (int i = scratch[31] + threadIdx.x; i < n; i += ROUTE_THREADS) order[i] = -1;
+    // scratch[31] still holds the number of kept slots: order past it is -1
+    for (int i = max(t0, scratch[31]) + threadIdx.x; i < t1; i += ROUTE_THREADS) order[i] = -1;
+}
+
+// Tiles of the slots: as many as there are SMs, of 1024 slots at least; one tile up to ROUTE_ONE slots.
+void route_tiles(long long n, int &tiles, int &tile)
+{
+    if (n <= ROUTE_ONE) { tiles = 1; tile = (int)n; return; }
+    const long long want = min((n + 1023) / 1024, 148ll);
+    tile = (int)(((n + want - 1) / want + 31) & ~31ll);
+    tiles = (int)((n + tile - 1) / tile);
 }
 
 __device__ __forceinline__ float to_f(float v) { return v; }
@@ -259,7 +314,9 @@ extern "C" {
 bls_status_t bls_moe_bytes(int64_t tokens, int k, int n_experts, size_t *bytes)
 {
     if (!bytes || !slots_ok(tokens, k, n_experts)) return BLS_EINVAL;
-    *bytes = 0;
+    int tiles, tile;
+    route_tiles(tokens * k, tiles, tile);
+    *bytes = tiles == 1 ? 0 : (sizeof(int) * tiles * n_experts + 255) / 256 * 256;
     return BLS_OK;
 }
 
@@ -269,11 +326,20 @@ bls_status_t bls_moe_route(const int32_t *expert, int64_t tokens, int k, int n_e
     size_t need = 0;
     if (bls_moe_bytes(tokens, k, n_experts, &need) != BLS_OK || !offsets || (tokens && (!expert || !order || !place))) return BLS_EINVAL;
     if (bytes < need) return BLS_ENOSPC;
-    (void)workspace;
-    const size_t smem = sizeof(int) * ROUTE_WARPS * n_experts;
-    if (cudaFuncSetAttribute(bls_moe_route_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return BLS_ECUDA;
-    return launch_serialised_smem(bls_moe_route_kernel, dim3(1), dim3(ROUTE_THREADS), smem, (cudaStream_t)cuda_stream, expert,
-                                  (int)(tokens * k), n_experts, order, place, offsets) == cudaSuccess ? BLS_OK : BLS_ECUDA;
+    if (need && (!workspace || ((uintptr_t)workspace & 255))) return BLS_EINVAL;
+    const int n = (int)(tokens * k);
+    int tiles, tile;
+    route_tiles(n, tiles, tile);
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    int *count = (int *)workspace;
+    auto kernel = tiles == 1 ? bls_moe_route_kernel<false> : bls_moe_route_kernel<true>;
+    const size_t smem = sizeof(int) * (ROUTE_WARPS + (tiles == 1 ? 0 : 2)) * n_experts;
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return BLS_ECUDA;
+    if (tiles > 1 && launch_serialised_smem(bls_moe_count_kernel, dim3(tiles), dim3(ROUTE_THREADS), sizeof(int) * n_experts, s, expert, n,
+                                            n_experts, tile, count) != cudaSuccess)
+        return BLS_ECUDA;
+    return launch_serialised_smem(kernel, dim3(tiles), dim3(ROUTE_THREADS), smem, s, expert, n, n_experts, tile, (const int *)count, order,
+                                  place, offsets) == cudaSuccess ? BLS_OK : BLS_ECUDA;
 }
 
 bls_status_t bls_moe_dispatch(const void *x, int64_t ldx, int dtype, const int32_t *place, const int32_t *offsets,

@@ -21,7 +21,7 @@ constexpr int GM_ROWS = 128;                                  // rows of x per t
 constexpr int GM_STAGES = 5;                                  // shared-memory stages of 128 inputs
 constexpr int GM_SLOTS = 4;                                   // tensor-memory slots of unpacked weights
 constexpr unsigned GM_X_BYTES = GM_ROWS * W4_TILE * 2, GM_STAGE_BYTES = GM_X_BYTES + W4_TILE_BYTES;
-constexpr int GM_THREADS = 18 * 32;
+constexpr int GM_THREADS = 20 * 32;                            // warps 18 and 19 only fill the fifth warpgroup
 constexpr unsigned GM_TMEM_COLS = 512, GM_A_COL = 256;        // accumulators: columns 0..127 and 128..255; weights: 4 x 64 columns
 constexpr int GM_MAX_E = 1024;
 
@@ -50,6 +50,18 @@ __device__ __forceinline__ void bulk_load(unsigned dst, const void *src, unsigne
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+// Registers move from the loading and unpacking warps to those that hold the running sums.  640 threads
+// start with 96 each (480 per five threads, one of each warpgroup); 2 x 80 + 2 x 136 + 40 = 472.
+template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// a * s + c on two fp32 values at once
+__device__ __forceinline__ unsigned long long fma2(unsigned long long s, unsigned a0, unsigned a1, unsigned long long c)
+{
+    unsigned long long r;
+    asm("{\n\t.reg .b64 a;\n\tmov.b64 a, {%2, %3};\n\tfma.rn.f32x2 %0, %1, a, %4;\n\t}" : "=l"(r) : "l"(s), "r"(a0), "r"(a1), "l"(c));
+    return r;
 }
 template <class T> __device__ __forceinline__ unsigned gm_idesc(int n)
 {
@@ -140,6 +152,7 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
     };
     const int gpt = W4_TILE / w.group;
 
+    if (warp >= 16) regs_down<40>();
     if (warp == 16) {
         if (lane == 0) {
             unsigned it = 0;
@@ -190,6 +203,7 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
             }
         }
     } else if (warp < 8) {
+        regs_down<80>();
         // unpack: thread = output row of the weight tile = lane of tensor memory
         const int q4 = warp & 3, set = warp >> 2, r = q4 * 32 + lane;
         const unsigned swz = (unsigned)((r >> 1) & 3);
@@ -198,12 +212,20 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
             const GmTile t = tile_of(i);
             const size_t z0 = (size_t)t.e * w.KT * gpt * w.NT * W4_TILE + t.nt * W4_TILE + r;
+            // the zero points of this set's next stage are on their way while a stage is unpacked
+            unsigned zn[4] = {8, 8, 8, 8};
+            auto fetch_zeros = [&](int kt) {
+                #pragma unroll
+                for (int b = 0; b < 4; b++)
+                    if (w.zero && kt < w.KT) zn[b] = w.zero[z0 + (size_t)(kt * gpt + b * 32 / w.group) * w.NT * W4_TILE];
+            };
+            fetch_zeros((it & 1) == (unsigned)set ? 0 : 1);
             for (int kt = 0; kt < w.KT; kt++, it++) {
                 if ((it & 1) != (unsigned)set) continue;
                 unsigned zp[4];
                 #pragma unroll
-                for (int b = 0; b < 4; b++)
-                    zp[b] = w4_zero_pair<T>(w.zero ? w.zero[z0 + (size_t)(kt * gpt + b * 32 / w.group) * w.NT * W4_TILE] & 15 : 8);
+                for (int b = 0; b < 4; b++) zp[b] = w4_zero_pair<T>(zn[b] & 15);
+                fetch_zeros(kt + 2);
                 const unsigned s = it % GM_STAGES, j = it % GM_SLOTS;
                 ok = mb_wait(full + 8 * s, (it / GM_STAGES) & 1, a.status) && mb_wait(a_empty + 8 * j, ((it / GM_SLOTS) & 1) ^ 1, a.status);
                 if (!ok) break;
@@ -236,7 +258,8 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                 }
             }
         }
-    } else {
+    } else if (warp < 16) {
+        regs_up<136>();
         // scale and store: thread = output, 64 rows of x each
         const int q4 = warp & 3, half = (warp - 8) >> 2;
         unsigned g = 0;
@@ -244,33 +267,51 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
             const GmTile t = tile_of(i);
             const int n = t.nt * W4_TILE + q4 * 32 + lane;
-            const __nv_bfloat16 *sc = w.scale + (size_t)t.e * w.KT * gpt * w.NT * W4_TILE + n;
+            const unsigned short *sc = (const unsigned short *)w.scale + (size_t)t.e * w.KT * gpt * w.NT * W4_TILE + n;
             const int groups = w.KT * gpt;
             const bool busy = half * 64 < t.rows;                          // the whole warp alike
-            float tot[64];
+            unsigned long long tot[32];                                    // two rows each
             #pragma unroll
-            for (int c = 0; c < 64; c++) tot[c] = 0.f;
-            for (int gi = 0; gi < groups; gi++, g++) {
-                const float s = __bfloat162float(sc[(size_t)gi * w.NT * W4_TILE]);
-                ok = mb_wait(d_full + 8 * (g & 1), (g >> 1) & 1, a.status);
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                if (busy) {
-                    const unsigned src = tmem + ((unsigned)(q4 * 32) << 16) + (g & 1) * 128 + half * 64;
-                    #pragma unroll
-                    for (int h = 0; h < 2; h++) {
-                        unsigned r[32];
-                        tmem_ld32(src + h * 32, r);
-                        if (h == 1) {
-                            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                            __syncwarp();
-                            if (lane == 0) mb_arrive(d_empty + 8 * (g & 1));
-                        }
+            for (int c = 0; c < 32; c++) tot[c] = 0ull;
+            // scales of the next four groups are on their way while four groups are added
+            unsigned short nx[4];
+            auto fetch_scales = [&](int gi) {
+                #pragma unroll
+                for (int b = 0; b < 4; b++)
+                    nx[b] = gi + b < groups ? __ldg(sc + (size_t)(gi + b) * w.NT * W4_TILE) : (unsigned short)0;
+            };
+            fetch_scales(0);
+            for (int g4 = 0; g4 < groups && ok; g4 += 4) {
+                unsigned short cur[4];
+                #pragma unroll
+                for (int b = 0; b < 4; b++) cur[b] = nx[b];
+                fetch_scales(g4 + 4);
+                #pragma unroll
+                for (int b = 0; b < 4; b++) {
+                    if (g4 + b >= groups) break;
+                    const unsigned si = (unsigned)cur[b] << 16;                   // bf16 -> fp32
+                    const unsigned long long s2 = (unsigned long long)si << 32 | si;
+                    ok = mb_wait(d_full + 8 * (g & 1), (g >> 1) & 1, a.status);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    if (busy) {
+                        const unsigned src = tmem + ((unsigned)(q4 * 32) << 16) + (g & 1) * 128 + half * 64;
                         #pragma unroll
-                        for (int c = 0; c < 32; c++) tot[h * 32 + c] = fmaf(s, __uint_as_float(r[c]), tot[h * 32 + c]);
+                        for (int h = 0; h < 2; h++) {
+                            unsigned r[32];
+                            tmem_ld32(src + h * 32, r);
+                            if (h == 1) {
+                                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                                __syncwarp();
+                                if (lane == 0) mb_arrive(d_empty + 8 * (g & 1));
+                            }
+                            #pragma unroll
+                            for (int c = 0; c < 16; c++) tot[h * 16 + c] = fma2(s2, r[2 * c], r[2 * c + 1], tot[h * 16 + c]);
+                        }
+                    } else if (lane == 0) {
+                        mb_arrive(d_empty + 8 * (g & 1));
                     }
-                } else if (lane == 0) {
-                    mb_arrive(d_empty + 8 * (g & 1));
+                    g++;
                 }
             }
             if (!ok || !busy || n >= w.N) continue;
@@ -278,7 +319,7 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
             #pragma unroll
             for (int c = 0; c < 64; c++) {
                 const int row = half * 64 + c;
-                if (row < t.rows) w4_store(a.y, (size_t)(t.row0 + row) * a.ldy + n, a.y_dtype, w4_act(tot[c] + bias, a.act));
+                if (row < t.rows) w4_store(a.y, (size_t)(t.row0 + row) * a.ldy + n, a.y_dtype, w4_act(__uint_as_float((unsigned)(tot[c >> 1] >> (32 * (c & 1)))) + bias, a.act));
             }
         }
     }

@@ -553,7 +553,7 @@ def test_calls_refuse_bad_arguments():
     assert lib.bls_w4_bytes(1, 8, 0, None, 8, 5, C.byref(n)) == bls.BLS_EINVAL
     assert bls.bls_w4_sizes(2, 129, 130, 64) == (2 * 2 * 2 * 8192, 2 * 2 * 2 * 2 * 128)
     # a misaligned q and a missing status word are refused by the library itself
-    p = t._ptrs
+    p = t._args
     args = lambda q, st: (q, p[1], None, 2, 40, 64, 32, x.data_ptr(), 2, 64, 5, o3.data_ptr(), None, 0, y.data_ptr(), 0, 40, None, 0, st, None)
     assert lib.bls_w4_linear(*args(p[0] + 8, o3.data_ptr())) == bls.BLS_EINVAL
     assert lib.bls_w4_linear(*args(p[0], None)) == bls.BLS_EINVAL
