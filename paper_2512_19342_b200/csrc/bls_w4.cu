@@ -126,59 +126,142 @@ __global__ void __launch_bounds__(MV_WARPS * 32) bls_w4_rows_kernel(W4Args a)
     }
 }
 
-__device__ __forceinline__ float w4_load(const void *p, size_t i, int dtype)
+template <int DT> struct W4Elem;
+template <> struct W4Elem<BLS_F32> { using type = float; };
+template <> struct W4Elem<BLS_BF16> { using type = __nv_bfloat16; };
+template <> struct W4Elem<BLS_F16> { using type = __half; };
+template <class T> struct alignas(16) W4Eight { T v[8]; };
+
+// Eight elements as loaded (16 or 32 bytes), and as fp32.
+template <class T> struct W4Raw { uint4 u[sizeof(T) / 2]; };
+template <class T, bool WHOLE>
+__device__ __forceinline__ W4Raw<T> w4_load8(const T *p, int avail)
 {
-    if (dtype == BLS_F32) return ((const float *)p)[i];
-    if (dtype == BLS_BF16) return __bfloat162float(((const __nv_bfloat16 *)p)[i]);
-    return __half2float(((const __half *)p)[i]);
+    W4Raw<T> r;
+    if (WHOLE && avail >= 8) {
+        #pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; i++) r.u[i] = ((const uint4 *)p)[i];
+        return r;
+    }
+    unsigned v[sizeof(T) * 2];
+    #pragma unroll
+    for (int i = 0; i < (int)sizeof(T) * 2; i++) v[i] = 0;
+    #pragma unroll
+    for (int i = 0; i < 8; i++)
+        if (i < avail) {
+            if (sizeof(T) == 4) v[i] = ((const unsigned *)p)[i];
+            else v[i >> 1] |= (unsigned)((const unsigned short *)p)[i] << (16 * (i & 1));
+        }
+    #pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; i++) r.u[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    return r;
+}
+__device__ __forceinline__ void w4_floats(const W4Raw<float> &r, float (&v)[8])
+{
+    #pragma unroll
+    for (int i = 0; i < 2; i++) {
+        v[4 * i] = __uint_as_float(r.u[i].x); v[4 * i + 1] = __uint_as_float(r.u[i].y);
+        v[4 * i + 2] = __uint_as_float(r.u[i].z); v[4 * i + 3] = __uint_as_float(r.u[i].w);
+    }
+}
+__device__ __forceinline__ void w4_floats(const W4Raw<__nv_bfloat16> &r, float (&v)[8])
+{
+    const unsigned u[4] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w};
+    #pragma unroll
+    for (int i = 0; i < 4; i++) { v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void w4_floats(const W4Raw<__half> &r, float (&v)[8])
+{
+    const unsigned u[4] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w};
+    #pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&u[i]));
+        v[2 * i] = f.x; v[2 * i + 1] = f.y;
+    }
 }
 
-// grid (KT, NT, E): one tile.  A warp takes an output row, a lane four neighbouring inputs, so that a
-// group is 8, 16 or 32 neighbouring lanes and a stored word two lanes.
-__global__ void __launch_bounds__(256) bls_w4_quantize_kernel(const void *w, int dtype, long long ldw, W4Weights d, uint8_t *q,
+// grid (KT, NT, E): one tile.  A lane takes the eight inputs of one stored word, half a warp an output row; a
+// group is 4, 8 or 16 neighbouring lanes.  A thread asks for four rows' pieces before it uses the
+// first.  WHOLE: rows of w start at 16-byte boundaries.
+//
+// The floor is reading w once, which leaves about 20 instructions per element.  So rint(w / s) of the
+// correctly rounded quotient comes from two products, with 1 / s made smaller and larger by 2^-19: a product is
+// within 1.5 2^-23 of the quotient relatively, so where both round to the same number it is the
+// right one.  Where they differ, fp32 inputs are divided.  16-bit inputs are then exactly halfway (w and
+// s have few bits; a quotient up to 15 that is no half stays 1e-4 away from one), which happens
+// often, and the even one of the two is right.  Adding 1.5 2^23 rounds a product to a whole number and
+// leaves it in the low bits; the constant's bits leave the sum of the eight nibbles at the end.
+template <int DT, bool WHOLE, bool ZERO>
+__global__ void __launch_bounds__(256) bls_w4_quantize_kernel(const void *wv, long long ldw, W4Weights d, uint8_t *q,
                                                               __nv_bfloat16 *scale, uint8_t *zero)
 {
+    using T = typename W4Elem<DT>::type;
     stream_order_enter();
     __shared__ __nv_bfloat16 s_sc[4][W4_TILE];
     __shared__ uint8_t s_z[4][W4_TILE];
     const int kt = blockIdx.x, nt = blockIdx.y, e = blockIdx.z;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int gpt = W4_TILE / d.group, lanes = d.group / 4;
+    const int l = threadIdx.x & 15;
+    const int gpt = W4_TILE / d.group, lanes = d.group / 8;
+    const int k = kt * W4_TILE + l * 8;
+    const T *w = (const T *)wv + ((size_t)e * d.N + nt * W4_TILE) * ldw + k;
     uint8_t *tile = q + (((size_t)e * d.NT + nt) * d.KT + kt) * W4_TILE_BYTES;
-    for (int r = warp; r < W4_TILE; r += 8) {
-        const int n = nt * W4_TILE + r, k = kt * W4_TILE + lane * 4;
-        float v[4], lo = 0.f, hi = 0.f;
-        bool bad = false;
+    #pragma unroll 1
+    for (int r0 = threadIdx.x >> 4; r0 < W4_TILE; r0 += 64) {
+        W4Raw<T> p[4];
         #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            v[i] = n < d.N && k + i < d.K ? w4_load(w, ((size_t)e * d.N + n) * ldw + k + i, dtype) : 0.f;
-            bad |= !isfinite(v[i]);
-            lo = fminf(lo, v[i]);
-            hi = fmaxf(hi, v[i]);
+        for (int u = 0; u < 4; u++) {
+            const int r = r0 + u * 16;
+            p[u] = w4_load8<T, WHOLE>(w + r * ldw, nt * W4_TILE + r < d.N ? d.K - k : 0);
         }
-        for (int o = 1; o < lanes; o <<= 1) {
-            lo = fminf(lo, __shfl_xor_sync(~0u, lo, o));
-            hi = fmaxf(hi, __shfl_xor_sync(~0u, hi, o));
-            bad |= __shfl_xor_sync(~0u, (int)bad, o) != 0;
-        }
-        const __nv_bfloat16 sb = bad ? __float2bfloat16_rn(__int_as_float(0x7fc00000)) :
-                                 __float2bfloat16_rn(zero ? __fdiv_rn(hi - lo, 15.f) : __fdiv_rn(fmaxf(hi, -lo), 7.f));
-        const float s = __bfloat162float(sb);
-        const bool usable = s > 0.f && isfinite(s);
-        const float z = !zero || n >= d.N ? 8.f : usable ? fminf(fmaxf(rintf(__fdiv_rn(-lo, s)), 0.f), 15.f) : 0.f;
-        unsigned word = 0;
         #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const float c = usable ? rintf(__fdiv_rn(v[i], s)) : 0.f;
-            const unsigned u = (unsigned)fminf(fmaxf(c + z, 0.f), 15.f);
-            word |= u << (4 * (((i >> 1) | ((lane & 1) << 1)) + 4 * (i & 1)));    // input i + 4 (lane mod 2) of the word
-        }
-        word |= __shfl_xor_sync(~0u, word, 1);
-        const int b = lane >> 3, t = (lane >> 1) & 3;
-        if ((lane & 1) == 0) *(unsigned *)(tile + r * 64 + (t ^ ((r >> 1) & 3)) * 16 + b * 4) = word;
-        if (lane % lanes == 0) {
-            s_sc[lane / lanes][r] = sb;
-            s_z[lane / lanes][r] = (uint8_t)z;
+        for (int u = 0; u < 4; u++) {
+            const int r = r0 + u * 16;
+            float v[8], lo = 0.f, hi = 0.f, bad = 0.f;                       // bad: NaN after a value that is not finite
+            w4_floats(p[u], v);
+            #pragma unroll
+            for (int i = 0; i < 8; i++) {
+                bad = fmaf(v[i], 0.f, bad);
+                if (ZERO) lo = fminf(lo, v[i]);
+                hi = fmaxf(hi, ZERO ? v[i] : fabsf(v[i]));
+            }
+            if (bad != 0.f) hi = __int_as_float(0x7f800000);
+            for (int o = 1; o < lanes; o <<= 1) {
+                if (ZERO) lo = fminf(lo, __shfl_xor_sync(~0u, lo, o));
+                hi = fmaxf(hi, __shfl_xor_sync(~0u, hi, o));
+            }
+            float s = __bfloat162float(__float2bfloat16_rn(ZERO ? __fdiv_rn(hi - lo, 15.f) : __fdiv_rn(hi, 7.f)));
+            if (!isfinite(s)) s = __int_as_float(0x7fc00000);                // the whole group becomes NaN
+            const __nv_bfloat16 sb = __float2bfloat16_rn(s);
+            const bool usable = s > 0.f;
+            const int z = !ZERO || nt * W4_TILE + r >= d.N ? 8 : usable ? (int)fminf(fmaxf(rintf(__fdiv_rn(-lo, s)), 0.f), 15.f) : 0;
+            // above 1e37 the reciprocal would be subnormal and lose bits
+            const float inv = usable && s < 1e37f ? __fdividef(1.f, s) : __int_as_float(0x7fc00000);
+            const float below = inv * (1.f - 0x1p-19f), above = inv * (1.f + 0x1p-19f);
+            constexpr float ROUND = 12582912.f;                              // 1.5 2^23
+            constexpr unsigned BITS = 0x4b400000u;                           // its bits
+            unsigned word = (unsigned)z * 0x11111111u - BITS * 0x11111111u, differ = 0;
+            #pragma unroll
+            for (int i = 0; i < 8; i++) {
+                unsigned t = __float_as_uint(fmaf(v[i], below, ROUND));
+                const unsigned t2 = __float_as_uint(fmaf(v[i], above, ROUND));
+                if (DT == BLS_F32) differ |= t ^ t2;
+                else if (t & 1) t = t2;
+                if (ZERO) t = min(t, BITS + 15u - z);                        // rint(w / s) + z is at least 0, but can reach 16
+                word += t << (4 * ((i >> 1) + 4 * (i & 1)));
+            }
+            if (differ || !(fmaxf(hi, -lo) * inv < (ZERO ? 15.5f : 7.5f))) {      // !(..): also where inv is NaN
+                word = 0;
+                #pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const int c = usable ? (int)rintf(__fdiv_rn(v[i], s)) : 0;
+                    word |= (unsigned)min(max(c + z, 0), 15) << (4 * ((i >> 1) + 4 * (i & 1)));
+                }
+            }
+            *(unsigned *)(tile + r * 64 + ((l & 3) ^ ((r >> 1) & 3)) * 16 + (l >> 2) * 4) = word;
+            if (l % lanes == 0) {
+                s_sc[l / lanes][r] = sb;
+                s_z[l / lanes][r] = (uint8_t)z;
+            }
         }
     }
     __syncthreads();
@@ -186,33 +269,62 @@ __global__ void __launch_bounds__(256) bls_w4_quantize_kernel(const void *w, int
         const int g = i / W4_TILE, r = i % W4_TILE;
         const size_t at = ((size_t)e * d.KT * gpt + kt * gpt + g) * d.NT * W4_TILE + nt * W4_TILE + r;
         scale[at] = s_sc[g][r];
-        if (zero) zero[at] = s_z[g][r];
+        if (ZERO) zero[at] = s_z[g][r];
     }
 }
 
-// grid (KT, NT, E): the inverse, with the same lanes.
-__global__ void __launch_bounds__(256) bls_w4_dequantize_kernel(W4Weights d, void *w, int dtype, long long ldw)
+// grid (KT, NT, E): the inverse, with the same lanes; bound by writing w once.
+template <int DT, bool WHOLE>
+__global__ void __launch_bounds__(256) bls_w4_dequantize_kernel(W4Weights d, void *wv, long long ldw)
 {
+    using T = typename W4Elem<DT>::type;
     stream_order_enter();
+    __shared__ float s_sc[4][W4_TILE];
+    __shared__ int s_z[4][W4_TILE];
     const int kt = blockIdx.x, nt = blockIdx.y, e = blockIdx.z;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int gpt = W4_TILE / d.group;
+    const int l = threadIdx.x & 15, gpt = W4_TILE / d.group;
+    const int k = kt * W4_TILE + l * 8, g = l * 8 / d.group;
     const uint8_t *tile = d.q + (((size_t)e * d.NT + nt) * d.KT + kt) * W4_TILE_BYTES;
-    for (int r = warp; r < W4_TILE; r += 8) {
-        const int n = nt * W4_TILE + r, k = kt * W4_TILE + lane * 4;
-        if (n >= d.N || k >= d.K) continue;
-        const int b = lane >> 3, t = (lane >> 1) & 3;
-        const unsigned word = *(const unsigned *)(tile + r * 64 + (t ^ ((r >> 1) & 3)) * 16 + b * 4);
-        const size_t sg = ((size_t)e * d.KT * gpt + kt * gpt + lane * 4 / d.group) * d.NT * W4_TILE + n;
-        const float s = __bfloat162float(d.scale[sg]);
-        const int z = d.zero ? d.zero[sg] & 15 : 8;
+    unsigned word[8];
+    #pragma unroll
+    for (int u = 0; u < 8; u++) {
+        const int r = (threadIdx.x >> 4) + u * 16;
+        word[u] = __ldg((const unsigned *)(tile + r * 64 + ((l & 3) ^ ((r >> 1) & 3)) * 16 + (l >> 2) * 4));
+    }
+    for (int i = threadIdx.x; i < gpt * W4_TILE; i += blockDim.x) {
+        const size_t at = ((size_t)e * d.KT * gpt + kt * gpt + i / W4_TILE) * d.NT * W4_TILE + nt * W4_TILE + i % W4_TILE;
+        s_sc[i / W4_TILE][i % W4_TILE] = __bfloat162float(d.scale[at]);
+        s_z[i / W4_TILE][i % W4_TILE] = d.zero ? d.zero[at] & 15 : 8;
+    }
+    __syncthreads();
+    T *w = (T *)wv + ((size_t)e * d.N + nt * W4_TILE) * ldw + k;
+    #pragma unroll
+    for (int u = 0; u < 8; u++) {
+        const int r = (threadIdx.x >> 4) + u * 16;
+        if (nt * W4_TILE + r >= d.N) break;
+        const float s = s_sc[g][r];
+        const int z = s_z[g][r];
+        W4Eight<T> o;
         #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int u = (word >> (4 * (((i >> 1) | ((lane & 1) << 1)) + 4 * (i & 1)))) & 15;
-            if (k + i < d.K) w4_store(w, ((size_t)e * d.N + n) * ldw + k + i, dtype, (float)(u - z) * s);
+        for (int i = 0; i < 8; i++) o.v[i] = T((float)((int)((word[u] >> (4 * ((i >> 1) + 4 * (i & 1)))) & 15) - z) * s);
+        if (WHOLE && k + 8 <= d.K) {
+            *(W4Eight<T> *)(w + r * ldw) = o;
+        } else {
+            #pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (k + i < d.K) w[r * ldw + i] = o.v[i];
         }
     }
 }
+
+// A kernel of one type with or without whole 16-byte pieces.
+#define W4_PICK(KERNEL, dtype, whole, ...)                                                                                        \
+    ((dtype) == BLS_F32 ? ((whole) ? KERNEL<BLS_F32, true __VA_ARGS__> : KERNEL<BLS_F32, false __VA_ARGS__>) :                        \
+     (dtype) == BLS_BF16 ? ((whole) ? KERNEL<BLS_BF16, true __VA_ARGS__> : KERNEL<BLS_BF16, false __VA_ARGS__>) :                     \
+                           ((whole) ? KERNEL<BLS_F16, true __VA_ARGS__> : KERNEL<BLS_F16, false __VA_ARGS__>))
+#define W4_COMMA ,
+
+bool w4_whole(const void *w, int dtype, long long ldw) { return ((uintptr_t)w & 15) == 0 && ldw * (dtype == BLS_F32 ? 4 : 2) % 16 == 0; }
 
 bool w4_shape(int E, int N, int K, int group, W4Weights &w)
 {
@@ -258,7 +370,9 @@ bls_status_t bls_w4_quantize(const void *w, int dtype, int64_t ldw, int E, int N
     W4Weights d = {};
     if (!w || !q || !scale || ((uintptr_t)q & 15) || dtype < 0 || dtype > 2 || ldw < K || !w4_shape(E, N, K, group, d)) return BLS_EINVAL;
     if (d.NT > 65535) return BLS_EINVAL;
-    return launch_serialised(bls_w4_quantize_kernel, dim3(d.KT, d.NT, E), dim3(256), (cudaStream_t)cuda_stream, w, dtype, ldw, d, q,
+    return launch_serialised(zero ? W4_PICK(bls_w4_quantize_kernel, dtype, w4_whole(w, dtype, ldw), W4_COMMA true) :
+                                    W4_PICK(bls_w4_quantize_kernel, dtype, w4_whole(w, dtype, ldw), W4_COMMA false), dim3(d.KT, d.NT, E), dim3(256),
+                             (cudaStream_t)cuda_stream, w, (long long)ldw, d, q,
                              (__nv_bfloat16 *)scale, zero) == cudaSuccess ? BLS_OK : BLS_ECUDA;
 }
 
@@ -268,7 +382,8 @@ bls_status_t bls_w4_dequantize(const uint8_t *q, const void *scale, const uint8_
     W4Weights d = {};
     if (!w || !q || !scale || ((uintptr_t)q & 15) || dtype < 0 || dtype > 2 || ldw < K || !w4_shape(E, N, K, group, d)) return BLS_EINVAL;
     d.q = q; d.scale = (const __nv_bfloat16 *)scale; d.zero = zero;
-    return launch_serialised(bls_w4_dequantize_kernel, dim3(d.KT, d.NT, E), dim3(256), (cudaStream_t)cuda_stream, d, w, dtype, ldw) ==
+    return launch_serialised(W4_PICK(bls_w4_dequantize_kernel, dtype, w4_whole(w, dtype, ldw)), dim3(d.KT, d.NT, E), dim3(256),
+                             (cudaStream_t)cuda_stream, d, w, (long long)ldw) ==
            cudaSuccess ? BLS_OK : BLS_ECUDA;
 }
 
