@@ -402,7 +402,7 @@ bls_status_t bls_w4_linear(const uint8_t *q, const void *scale, const uint8_t *z
 {
     W4Args a = {};
     size_t need = 0;
-    if (!q || !scale || ((uintptr_t)q & 15) || !w4_shape(E, N, K, group, a.w) || bls_w4_bytes(E, N, K, x, ldx, rows, &need) != BLS_OK ||
+    if (!q || !scale || (((uintptr_t)q | (uintptr_t)scale | (uintptr_t)zero) & 15) || !w4_shape(E, N, K, group, a.w) || bls_w4_bytes(E, N, K, x, ldx, rows, &need) != BLS_OK ||
         (x_dtype != BLS_BF16 && x_dtype != BLS_F16) || y_dtype < 0 || y_dtype > 2 || act < 0 || act > 2 || ldx < K || ldy < N ||
         (!offsets && E != 1) || (rows && (!x || !y)) || !status)
         return BLS_EINVAL;

@@ -37,6 +37,11 @@ __device__ __forceinline__ float w4_act(float v, int act)
     return v;
 }
 
+template <class Y> __device__ __forceinline__ Y from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+
 __device__ __forceinline__ void w4_store(void *y, size_t i, int dtype, float v)
 {
     if (dtype == BLS_F32) ((float *)y)[i] = v;

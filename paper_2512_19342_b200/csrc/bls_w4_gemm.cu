@@ -1,29 +1,37 @@
 // The 4-bit product for many rows, on the tensor cores.
 //
-// A CTA computes 128 outputs x 128 rows: the weights are the M operand, unpacked by warps from
+// A CTA computes 128 outputs x 128 or 256 rows: the weights are the M operand, unpacked by warps from
 // shared memory into tensor memory (integers q - z, exact in bf16 and f16), the rows of x are the
 // N operand in shared memory.  The accumulator of one group of inputs is complete after group / 16
 // instructions; it is then read back, scaled in fp32 and added to the running sums in registers,
-// while the next group accumulates in a second buffer.  Weights are therefore never rounded, and
-// a thread needs one scale per group, because its accumulator lane is one output.
+// while the next one (the other half of the rows, or the next group) accumulates in a second buffer.
+// Weights are therefore never rounded, and a thread needs one scale per group, because its
+// accumulator lane is one output.
 //
-// Roles: warps 0-7 unpack (two sets of four take the stages in turn), warps 8-15 scale and
-// store, one thread of warp 16 loads (TMA for x, one bulk copy per stored weight tile), one thread
-// of warp 17 issues the products.  Every wait is bounded by the clock: one that gives up latches
-// BLS_ST_ETIMEOUT, all roles wind down and tensor memory is released.
+// Roles: warps 0-3 unpack, warps 4-11 scale and store, one thread of warp 12 loads (TMA for x, bulk
+// copies for the weight tile and its scales and zero points), one thread of warp 13 issues the
+// products.  Every wait is bounded by the clock: one that gives up latches BLS_ST_ETIMEOUT, all
+// roles wind down and tensor memory is released.
 #include "bls_tc.cuh"
 #include "bls_w4.cuh"
 #include "bls_w4_gemm.h"
 
 namespace {
 
-constexpr int GM_ROWS = 128;                                  // rows of x per tile (N of the instruction)
-constexpr int GM_STAGES = 5;                                  // shared-memory stages of 128 inputs
+constexpr int GM_HALF = 128;                                  // rows of x per product instruction (its N)
 constexpr int GM_SLOTS = 4;                                   // tensor-memory slots of unpacked weights
-constexpr unsigned GM_X_BYTES = GM_ROWS * W4_TILE * 2, GM_STAGE_BYTES = GM_X_BYTES + W4_TILE_BYTES;
-constexpr int GM_THREADS = 20 * 32;                            // warps 18 and 19 only fill the fifth warpgroup
+constexpr unsigned GM_HALF_BYTES = GM_HALF * W4_TILE * 2;     // one stage's x of 128 rows: two boxes of 64 inputs
+constexpr int GM_THREADS = 16 * 32;                           // warps 14 and 15 only fill the fourth warpgroup
 constexpr unsigned GM_TMEM_COLS = 512, GM_A_COL = 256;        // accumulators: columns 0..127 and 128..255; weights: 4 x 64 columns
 constexpr int GM_MAX_E = 1024;
+
+// A stage of 128 inputs: x, the weight tile, the scales and the zero points of its groups.
+template <int HALVES> struct GmStage {
+    static constexpr int COUNT = HALVES == 2 ? 3 : 5;         // what fits into 227 KB
+    static constexpr unsigned W = HALVES * GM_HALF_BYTES, BYTES = W + W4_TILE_BYTES;                        // x, weights
+    static constexpr unsigned SCALE = COUNT * BYTES, ZERO = 4 * W4_TILE * 2, SIDE = 4 * W4_TILE * 3;        // after all stages: scales, zero points
+    static constexpr unsigned ALL = COUNT * (BYTES + SIDE);
+};
 
 struct GmTile { int e, row0, rows, nt; };                     // matrix, first row, rows of x in the tile, output tile
 
@@ -51,8 +59,14 @@ __device__ __forceinline__ void bulk_load(unsigned dst, const void *src, unsigne
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-// Registers move from the loading and unpacking warps to those that hold the running sums.  640 threads
-// start with 96 each (480 per five threads, one of each warpgroup); 2 x 80 + 2 x 136 + 40 = 472.
+__device__ __forceinline__ bool elect_one()
+{
+    unsigned p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+// Registers move to the warps that hold the running sums: 512 threads start with 128 each (512 per four
+// threads, one of each warpgroup); 80 + 2 x 200 + 32 = 512.
 template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 
@@ -65,47 +79,63 @@ __device__ __forceinline__ unsigned long long fma2(unsigned long long s, unsigne
 }
 template <class T> __device__ __forceinline__ unsigned gm_idesc(int n)
 {
-    constexpr unsigned f = sizeof(T) == 2 && W4Pairs<T>::MAGIC == 0x43004300u ? 1u : 0u;      // 1 bf16, 0 f16
+    constexpr unsigned f = W4Pairs<T>::MAGIC == 0x43004300u ? 1u : 0u;                        // 1 bf16, 0 f16
     return (1u << 4) | (f << 7) | (f << 10) | ((unsigned)(n >> 3) << 17) | ((unsigned)(128 >> 4) << 24);
 }
 
-// grid: persistent, one CTA per SM at most; tiles are numbered over (matrix, row tile, output tile).
-template <class T>
-__global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __grid_constant__ CUtensorMap map_x, W4Args a)
+// 32 results of one output, one per row of x, from `at` on.
+template <class Y>
+__device__ __forceinline__ void gm_store(Y *at, long long ldy, int rows, const unsigned long long (&tot)[16], float bias, int act)
 {
+    #pragma unroll
+    for (int c = 0; c < 32; c++) {
+        float v = __uint_as_float((unsigned)(tot[c >> 1] >> (32 * (c & 1)))) + bias;
+        if (act) v = w4_act(v, act);
+        if (c < rows) *at = from_float<Y>(v);
+        at += ldy;
+    }
+}
+
+// grid: persistent, one CTA per SM at most; tiles are numbered over (matrix, row tile, output tile).
+template <class T, int GROUP, int HALVES>
+__global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ W4Args a)
+{
+    using Stage = GmStage<HALVES>;
+    constexpr int STAGES = Stage::COUNT, GPT = W4_TILE / GROUP, ROWS = HALVES * GM_HALF;
     extern __shared__ unsigned char gm_smem[];
-    __shared__ __align__(8) unsigned long long bars[2 * GM_STAGES + 2 * GM_SLOTS + 4];
+    __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * GM_SLOTS + 4];
     __shared__ unsigned tmem_slot;
     __shared__ int tile_end[GM_MAX_E];                            // row tiles of the matrices up to and including this one
-    __shared__ int scan[32];
+    __shared__ int scan[16];
     const unsigned smem = (s_addr(gm_smem) + 1023u) & ~1023u;
-    const unsigned full = s_addr(&bars[0]), empty = full + 8 * GM_STAGES, a_full = empty + 8 * GM_STAGES, a_empty = a_full + 8 * GM_SLOTS,
+    const unsigned full = s_addr(&bars[0]), empty = full + 8 * STAGES, a_full = empty + 8 * STAGES, a_empty = a_full + 8 * GM_SLOTS,
                    d_full = a_empty + 8 * GM_SLOTS, d_empty = d_full + 16;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const W4Weights &w = a.w;
+    const int KT = w.KT;
 
     if (threadIdx.x == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
-        for (int s = 0; s < GM_STAGES; s++) { mb_init(full + 8 * s, 1); mb_init(empty + 8 * s, 1 + 4); }
+        for (int s = 0; s < STAGES; s++) { mb_init(full + 8 * s, 1); mb_init(empty + 8 * s, 1 + 4 + 8); }
         for (int s = 0; s < GM_SLOTS; s++) { mb_init(a_full + 8 * s, 4); mb_init(a_empty + 8 * s, 1); }
         for (int s = 0; s < 2; s++) { mb_init(d_full + 8 * s, 1); mb_init(d_empty + 8 * s, 8); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == 17) {
+    if (warp == 13) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s_addr(&tmem_slot)), "r"(GM_TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     stream_order_enter();
-    // row tiles of every matrix, summed up: the first E threads count, a scan over chunks of 512 adds
+    // row tiles of every matrix, summed up in chunks of one matrix per thread
     int carry = 0;
-    for (int e0 = 0; e0 < w.E; e0 += 512) {
+    for (int e0 = 0; e0 < w.E; e0 += GM_THREADS) {
         const int e = e0 + threadIdx.x;
         int c = 0;
-        if (threadIdx.x < 512 && e < w.E) {
+        if (e < w.E) {
             int lo, hi;
             w4_rows(a, e, lo, hi);
-            c = (hi - lo + GM_ROWS - 1) / GM_ROWS;
+            c = (hi - lo + ROWS - 1) / ROWS;
         }
         #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -114,13 +144,13 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         }
         if (lane == 31) scan[warp] = c;
         __syncthreads();
-        int before = carry, all = carry;
+        int before = carry;
+        #pragma unroll
         for (int i = 0; i < 16; i++) {
             if (i < warp) before += scan[i];
-            all += scan[i];
+            carry += scan[i];
         }
-        if (threadIdx.x < 512 && e < w.E) tile_end[e] = before + c;
-        carry = all;
+        if (e < w.E) tile_end[e] = before + c;
         __syncthreads();
     }
     if (a.offsets) {                                               // rows of no matrix become 0
@@ -146,104 +176,127 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         t.nt = i % w.NT;
         int r0, r1;
         w4_rows(a, lo, r0, r1);
-        t.row0 = r0 + (m - (lo ? tile_end[lo - 1] : 0)) * GM_ROWS;
-        t.rows = min(GM_ROWS, r1 - t.row0);
+        t.row0 = r0 + (m - (lo ? tile_end[lo - 1] : 0)) * ROWS;
+        t.rows = min(ROWS, r1 - t.row0);
         return t;
     };
-    const int gpt = W4_TILE / w.group;
 
-    if (warp >= 16) regs_down<40>();
-    if (warp == 16) {
-        if (lane == 0) {
-            unsigned it = 0;
+    if (warp >= 12) {
+        regs_down<32>();
+        if (warp == 12 && lane == 0) {
+            unsigned s = 0, ph = 0, issued = 0;
             bool ok = true;
             for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
                 const GmTile t = tile_of(i);
-                const uint8_t *q = w.q + ((size_t)t.e * w.NT + t.nt) * w.KT * W4_TILE_BYTES;
-                for (int kt = 0; kt < w.KT; kt++, it++) {
-                    const unsigned s = it % GM_STAGES;
-                    ok = mb_wait(empty + 8 * s, ((it / GM_STAGES) & 1) ^ 1, a.status);
+                const uint8_t *q = w.q + ((size_t)t.e * w.NT + t.nt) * KT * W4_TILE_BYTES;
+                size_t g = (size_t)t.e * KT * GPT * w.NT * W4_TILE + t.nt * W4_TILE;
+                const bool two = HALVES == 2 && t.rows > GM_HALF;
+                const unsigned bytes = W4_TILE_BYTES + (two ? 2 : 1) * GM_HALF_BYTES + GPT * W4_TILE * (w.zero ? 3 : 2);
+                for (int kt = 0; kt < KT; kt++) {
+                    ok = mb_wait(empty + 8 * s, ph ^ 1, a.status);
                     if (!ok) break;
-                    const unsigned dst = smem + s * GM_STAGE_BYTES, bar = full + 8 * s;
-                    mb_expect_tx(bar, GM_STAGE_BYTES);
-                    bulk_load(dst + GM_X_BYTES, q + (size_t)kt * W4_TILE_BYTES, W4_TILE_BYTES, bar);
+                    const unsigned dst = smem + s * Stage::BYTES, side = smem + Stage::SCALE + s * Stage::SIDE, bar = full + 8 * s;
+                    mb_expect_tx(bar, bytes);
+                    bulk_load(dst + Stage::W, q, W4_TILE_BYTES, bar);
+                    q += W4_TILE_BYTES;
                     tma_load_2d(dst, &map_x, bar, kt * W4_TILE, t.row0);
-                    tma_load_2d(dst + GM_X_BYTES / 2, &map_x, bar, kt * W4_TILE + 64, t.row0);
+                    tma_load_2d(dst + GM_HALF_BYTES / 2, &map_x, bar, kt * W4_TILE + 64, t.row0);
+                    if (two) {
+                        tma_load_2d(dst + GM_HALF_BYTES, &map_x, bar, kt * W4_TILE, t.row0 + GM_HALF);
+                        tma_load_2d(dst + GM_HALF_BYTES + GM_HALF_BYTES / 2, &map_x, bar, kt * W4_TILE + 64, t.row0 + GM_HALF);
+                    }
+                    #pragma unroll
+                    for (int gi = 0; gi < GPT; gi++) {
+                        bulk_load(side + gi * W4_TILE * 2, w.scale + g, W4_TILE * 2, bar);
+                        if (w.zero) bulk_load(side + Stage::ZERO + gi * W4_TILE, w.zero + g, W4_TILE, bar);
+                        g += (size_t)w.NT * W4_TILE;
+                    }
+                    issued++;
+                    if (++s == STAGES) { s = 0; ph ^= 1; }
                 }
             }
             // the copies still in flight write to this CTA's shared memory: see them land before leaving
-            for (unsigned b = it > GM_STAGES ? it - GM_STAGES : 0; b < it; b++) mb_wait(full + 8 * (b % GM_STAGES), (b / GM_STAGES) & 1, a.status);
-        }
-    } else if (warp == 17) {
-        if (lane == 0) {
-            unsigned it = 0, g = 0;
+            for (unsigned b = issued > STAGES ? issued - STAGES : 0; b < issued; b++) mb_wait(full + 8 * (b % STAGES), (b / STAGES) & 1, a.status);
+        } else if (warp == 13) {
+            // the whole warp follows, one thread of it issues
+            const bool leader = elect_one();
+            unsigned s = 0, ph = 0, j = 0, jph = 0, used[2] = {0, 0}, b = 0;
             bool ok = true;
             for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
                 const GmTile t = tile_of(i);
-                const unsigned idesc = gm_idesc<T>((t.rows + 15) & ~15);
-                for (int kt = 0; kt < w.KT && ok; kt++, it++) {
-                    const unsigned s = it % GM_STAGES, j = it % GM_SLOTS;
-                    ok = mb_wait(full + 8 * s, (it / GM_STAGES) & 1, a.status) && mb_wait(a_full + 8 * j, (it / GM_SLOTS) & 1, a.status);
+                for (int kt = 0; kt < KT && ok; kt++) {
+                    ok = mb_wait(full + 8 * s, ph, a.status) && mb_wait(a_full + 8 * j, jph, a.status);
                     if (!ok) break;
-                    for (int gi = 0; gi < gpt && ok; gi++, g++) {
-                        ok = mb_wait(d_empty + 8 * (g & 1), ((g >> 1) & 1) ^ 1, a.status);
-                        if (!ok) break;
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const int steps = w.group / 16;
-                        for (int k = 0; k < steps; k++) {
-                            const int ks = gi * steps + k;            // step of 16 inputs in the stage: half-tile ks / 4, 32 bytes each
-                            umma_f16_ta(tmem + (g & 1) * 128, tmem + GM_A_COL + j * 64 + ks * 8,
-                                        umma_desc(smem + s * GM_STAGE_BYTES + (ks >> 2) * (GM_X_BYTES / 2) + (ks & 3) * 32), idesc, k ? 1u : 0u);
+                    const unsigned long long base = umma_desc(smem + s * Stage::BYTES);
+                    const unsigned at = tmem + GM_A_COL + j * 64;
+                    #pragma unroll
+                    for (int gi = 0; gi < GPT; gi++) {
+                        #pragma unroll
+                        for (int h = 0; h < HALVES; h++) {
+                            const int rows = min(GM_HALF, t.rows - h * GM_HALF);
+                            if (rows <= 0) continue;
+                            if (HALVES == 2) b = h;
+                            ok = ok && mb_wait(d_empty + 8 * b, (used[HALVES == 2 ? h : 0] & 1) ^ 1, a.status);
+                            if (HALVES == 2 || b == 1) used[HALVES == 2 ? h : 0]++;   // how often the buffer (HALVES == 1: both) has been filled
+                            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                            if (leader && ok) {
+                                const unsigned idesc = gm_idesc<T>((rows + 15) & ~15);
+                                #pragma unroll
+                                for (int k = 0; k < GROUP / 16; k++) {
+                                    const int ks = gi * (GROUP / 16) + k;     // step of 16 inputs: box ks / 4, 32 bytes each
+                                    umma_f16_ta(tmem + b * 128, at + ks * 8,
+                                                base + (h * GM_HALF_BYTES + (ks >> 2) * (GM_HALF_BYTES / 2) + (ks & 3) * 32) / 16, idesc, k ? 1u : 0u);
+                                }
+                                umma_commit(d_full + 8 * b);
+                            }
+                            if (HALVES == 1) b ^= 1;
                         }
-                        umma_commit(d_full + 8 * (g & 1));
                     }
-                    umma_commit(a_empty + 8 * j);
-                    umma_commit(empty + 8 * s);
+                    if (leader && ok) {
+                        umma_commit(a_empty + 8 * j);
+                        umma_commit(empty + 8 * s);
+                    }
+                    __syncwarp();
+                    if (++s == STAGES) { s = 0; ph ^= 1; }
+                    if (++j == GM_SLOTS) { j = 0; jph ^= 1; }
                 }
             }
         }
-    } else if (warp < 8) {
+    } else if (warp < 4) {
         regs_down<80>();
         // unpack: thread = output row of the weight tile = lane of tensor memory
-        const int q4 = warp & 3, set = warp >> 2, r = q4 * 32 + lane;
+        const int r = warp * 32 + lane;
         const unsigned swz = (unsigned)((r >> 1) & 3);
-        unsigned it = 0;
+        unsigned s = 0, ph = 0, j = 0, jph = 0;
         bool ok = true;
         for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-            const GmTile t = tile_of(i);
-            const size_t z0 = (size_t)t.e * w.KT * gpt * w.NT * W4_TILE + t.nt * W4_TILE + r;
-            // the zero points of this set's next stage are on their way while a stage is unpacked
-            unsigned zn[4] = {8, 8, 8, 8};
-            auto fetch_zeros = [&](int kt) {
-                #pragma unroll
-                for (int b = 0; b < 4; b++)
-                    if (w.zero && kt < w.KT) zn[b] = w.zero[z0 + (size_t)(kt * gpt + b * 32 / w.group) * w.NT * W4_TILE];
-            };
-            fetch_zeros((it & 1) == (unsigned)set ? 0 : 1);
-            for (int kt = 0; kt < w.KT; kt++, it++) {
-                if ((it & 1) != (unsigned)set) continue;
-                unsigned zp[4];
-                #pragma unroll
-                for (int b = 0; b < 4; b++) zp[b] = w4_zero_pair<T>(zn[b] & 15);
-                fetch_zeros(kt + 2);
-                const unsigned s = it % GM_STAGES, j = it % GM_SLOTS;
-                ok = mb_wait(full + 8 * s, (it / GM_STAGES) & 1, a.status) && mb_wait(a_empty + 8 * j, ((it / GM_SLOTS) & 1) ^ 1, a.status);
+            for (int kt = 0; kt < KT; kt++) {
+                ok = mb_wait(full + 8 * s, ph, a.status);
                 if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const unsigned src = smem + s * GM_STAGE_BYTES + GM_X_BYTES + r * 64;
+                const unsigned src = smem + s * Stage::BYTES + Stage::W + r * 64;
                 unsigned word[4][4];                                      // [quarter][block of 32 inputs]
                 #pragma unroll
                 for (int p = 0; p < 4; p++)
                     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                                  : "=r"(word[p][0]), "=r"(word[p][1]), "=r"(word[p][2]), "=r"(word[p][3]) : "r"(src + ((p ^ swz) * 16)));
-                const unsigned dst = tmem + ((unsigned)(q4 * 32) << 16) + GM_A_COL + j * 64;
+                unsigned zp[GPT];
+                #pragma unroll
+                for (int gi = 0; gi < GPT; gi++) {
+                    unsigned z = 8;
+                    if (w.zero) asm volatile("ld.shared.u8 %0, [%1];" : "=r"(z) : "r"(smem + Stage::SCALE + s * Stage::SIDE + Stage::ZERO + gi * W4_TILE + r));
+                    zp[gi] = w4_zero_pair<T>(z & 15);
+                }
+                ok = mb_wait(a_empty + 8 * j, jph ^ 1, a.status);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const unsigned dst = tmem + ((unsigned)(warp * 32) << 16) + GM_A_COL + j * 64;
                 #pragma unroll
                 for (int b = 0; b < 4; b++) {
                     unsigned o[16];
                     #pragma unroll
                     for (int p = 0; p < 4; p++) {
                         unsigned v[4];
-                        w4_unpack<T>(word[p][b], zp[b], v);
+                        w4_unpack<T>(word[p][b], zp[b * 32 / GROUP], v);
                         #pragma unroll
                         for (int c = 0; c < 4; c++) o[p * 4 + c] = v[c];
                     }
@@ -256,76 +309,84 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                     mb_arrive(a_full + 8 * j);
                     mb_arrive(empty + 8 * s);
                 }
+                if (++s == STAGES) { s = 0; ph ^= 1; }
+                if (++j == GM_SLOTS) { j = 0; jph ^= 1; }
             }
         }
-    } else if (warp < 16) {
-        regs_up<136>();
-        // scale and store: thread = output, 64 rows of x each
-        const int q4 = warp & 3, half = (warp - 8) >> 2;
-        unsigned g = 0;
+    } else {
+        regs_up<200>();
+        // scale and store: thread = output, 64 rows of x of every half
+        const int q4 = warp & 3, part = (warp - 4) >> 2, r = q4 * 32 + lane;
+        const unsigned lanes = (unsigned)(q4 * 32) << 16;
+        unsigned s = 0, ph = 0, used[2] = {0, 0}, b = 0;
         bool ok = true;
         for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
             const GmTile t = tile_of(i);
-            const int n = t.nt * W4_TILE + q4 * 32 + lane;
-            const unsigned short *sc = (const unsigned short *)w.scale + (size_t)t.e * w.KT * gpt * w.NT * W4_TILE + n;
-            const int groups = w.KT * gpt;
-            const bool busy = half * 64 < t.rows;                          // the whole warp alike
-            unsigned long long tot[32];                                    // two rows each
+            unsigned long long tot[HALVES][2][16];                         // two rows each
             #pragma unroll
-            for (int c = 0; c < 32; c++) tot[c] = 0ull;
-            // scales of the next four groups are on their way while four groups are added
-            unsigned short nx[4];
-            auto fetch_scales = [&](int gi) {
+            for (int h = 0; h < HALVES; h++)
                 #pragma unroll
-                for (int b = 0; b < 4; b++)
-                    nx[b] = gi + b < groups ? __ldg(sc + (size_t)(gi + b) * w.NT * W4_TILE) : (unsigned short)0;
-            };
-            fetch_scales(0);
-            for (int g4 = 0; g4 < groups && ok; g4 += 4) {
-                unsigned short cur[4];
+                for (int c = 0; c < 32; c++) tot[h][c >> 4][c & 15] = 0ull;
+            for (int kt = 0; kt < KT && ok; kt++) {
+                ok = mb_wait(full + 8 * s, ph, a.status);                  // the scales have arrived
+                if (!ok) break;
+                unsigned sc[GPT];
                 #pragma unroll
-                for (int b = 0; b < 4; b++) cur[b] = nx[b];
-                fetch_scales(g4 + 4);
+                for (int gi = 0; gi < GPT; gi++)
+                    asm volatile("{\n\t.reg .u16 h;\n\tld.shared.u16 h, [%1];\n\tmov.b32 %0, {0, h};\n\t}" : "=r"(sc[gi])
+                                 : "r"(smem + Stage::SCALE + s * Stage::SIDE + gi * W4_TILE * 2 + r * 2));      // bf16 -> fp32
+                __syncwarp();
+                if (lane == 0) mb_arrive(empty + 8 * s);
                 #pragma unroll
-                for (int b = 0; b < 4; b++) {
-                    if (g4 + b >= groups) break;
-                    const unsigned si = (unsigned)cur[b] << 16;                   // bf16 -> fp32
-                    const unsigned long long s2 = (unsigned long long)si << 32 | si;
-                    ok = mb_wait(d_full + 8 * (g & 1), (g >> 1) & 1, a.status);
-                    if (!ok) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    if (busy) {
-                        const unsigned src = tmem + ((unsigned)(q4 * 32) << 16) + (g & 1) * 128 + half * 64;
-                        #pragma unroll
-                        for (int h = 0; h < 2; h++) {
-                            unsigned r[32];
-                            tmem_ld32(src + h * 32, r);
-                            if (h == 1) {
-                                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                                __syncwarp();
-                                if (lane == 0) mb_arrive(d_empty + 8 * (g & 1));
-                            }
+                for (int gi = 0; gi < GPT; gi++) {
+                    const unsigned long long s2 = (unsigned long long)sc[gi] << 32 | sc[gi];
+                    #pragma unroll
+                    for (int h = 0; h < HALVES; h++) {
+                        if (h * GM_HALF >= t.rows) continue;
+                        if (HALVES == 2) b = h;
+                        ok = ok && mb_wait(d_full + 8 * b, used[HALVES == 2 ? h : 0] & 1, a.status);
+                        if (HALVES == 2 || b == 1) used[HALVES == 2 ? h : 0]++;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const bool busy = ok && h * GM_HALF + part * 64 < t.rows;          // the whole warp alike
+                        const unsigned src = tmem + lanes + b * 128 + part * 64;
+                        unsigned v[32];
+                        if (busy) {
+                            tmem_ld32(src, v);
                             #pragma unroll
-                            for (int c = 0; c < 16; c++) tot[h * 16 + c] = fma2(s2, r[2 * c], r[2 * c + 1], tot[h * 16 + c]);
+                            for (int c = 0; c < 16; c++) tot[h][0][c] = fma2(s2, v[2 * c], v[2 * c + 1], tot[h][0][c]);
+                            tmem_ld32(src + 32, v);
                         }
-                    } else if (lane == 0) {
-                        mb_arrive(d_empty + 8 * (g & 1));
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) mb_arrive(d_empty + 8 * b);
+                        if (busy) {
+                            #pragma unroll
+                            for (int c = 0; c < 16; c++) tot[h][1][c] = fma2(s2, v[2 * c], v[2 * c + 1], tot[h][1][c]);
+                        }
+                        if (HALVES == 1) b ^= 1;
                     }
-                    g++;
                 }
+                if (++s == STAGES) { s = 0; ph ^= 1; }
             }
-            if (!ok || !busy || n >= w.N) continue;
+            const int n = t.nt * W4_TILE + r;
+            if (!ok || n >= w.N) continue;
             const float bias = a.bias ? a.bias[(size_t)t.e * w.N + n] : 0.f;
             #pragma unroll
-            for (int c = 0; c < 64; c++) {
-                const int row = half * 64 + c;
-                if (row < t.rows) w4_store(a.y, (size_t)(t.row0 + row) * a.ldy + n, a.y_dtype, w4_act(__uint_as_float((unsigned)(tot[c >> 1] >> (32 * (c & 1)))) + bias, a.act));
-            }
+            for (int h = 0; h < HALVES; h++)
+                #pragma unroll
+                for (int p = 0; p < 2; p++) {
+                    const int row = h * GM_HALF + part * 64 + p * 32;
+                    if (row >= t.rows) continue;
+                    const size_t at = (size_t)(t.row0 + row) * a.ldy + n;
+                    if (a.y_dtype == BLS_F32) gm_store((float *)a.y + at, a.ldy, t.rows - row, tot[h][p], bias, a.act);
+                    else if (a.y_dtype == BLS_BF16) gm_store((__nv_bfloat16 *)a.y + at, a.ldy, t.rows - row, tot[h][p], bias, a.act);
+                    else gm_store((__half *)a.y + at, a.ldy, t.rows - row, tot[h][p], bias, a.act);
+                }
         }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (warp == 17) {
+    if (warp == 13) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(GM_TMEM_COLS) : "memory");
     }
@@ -357,16 +418,31 @@ int sm_count()
     return n > 0 ? n : 148;
 }
 
+template <class T, int GROUP, int HALVES>
+cudaError_t launch_tiles_h(const CUtensorMap &map, const W4Args &a, long long row_tiles, cudaStream_t s)
+{
+    const size_t smem = 1024 + (size_t)GmStage<HALVES>::ALL;
+    cudaError_t e = cudaFuncSetAttribute(bls_w4_tiles_kernel<T, GROUP, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    const int grid = (int)min(row_tiles * a.w.NT, (long long)sm_count());
+    return launch_serialised_smem(bls_w4_tiles_kernel<T, GROUP, HALVES>, dim3(grid), dim3(GM_THREADS), smem, s, map, a);
+}
+
+template <class T, int GROUP>
+cudaError_t launch_tiles_g(const CUtensorMap &map, const W4Args &a, cudaStream_t s)
+{
+    // tiles of 256 rows unpack every weight for twice as many products; they are taken where enough of them remain
+    const long long big = (a.rows + 255) / 256;
+    const bool two = big * a.w.NT >= 2ll * sm_count();
+    // an upper bound of the row tiles: every matrix may end in a part of one
+    const long long per = two ? 256 : 128, row_tiles = (a.rows + per - 1) / per + (a.offsets ? min((long long)a.w.E, (long long)a.rows) : 0);
+    return two ? launch_tiles_h<T, GROUP, 2>(map, a, row_tiles, s) : launch_tiles_h<T, GROUP, 1>(map, a, row_tiles, s);
+}
+
 template <class T>
 cudaError_t launch_tiles(const CUtensorMap &map, const W4Args &a, cudaStream_t s)
 {
-    const size_t smem = 1024 + (size_t)GM_STAGES * GM_STAGE_BYTES;
-    cudaError_t e = cudaFuncSetAttribute(bls_w4_tiles_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    // an upper bound of the tiles: every matrix may end in a part of one
-    const long long row_tiles = a.offsets ? min((long long)a.rows, (a.rows + GM_ROWS - 1) / GM_ROWS + (long long)a.w.E) : (a.rows + GM_ROWS - 1) / GM_ROWS;
-    const int grid = (int)min(row_tiles * a.w.NT, (long long)sm_count());
-    return launch_serialised_smem(bls_w4_tiles_kernel<T>, dim3(grid), dim3(GM_THREADS), smem, s, map, a);
+    return a.w.group == 32 ? launch_tiles_g<T, 32>(map, a, s) : a.w.group == 64 ? launch_tiles_g<T, 64>(map, a, s) : launch_tiles_g<T, 128>(map, a, s);
 }
 
 }  // namespace
@@ -388,6 +464,6 @@ cudaError_t w4_tiles(W4Args a, int x_dtype, void *workspace, cudaStream_t s)
         a.x = workspace; a.ldx = ldo; a.x_pieces = 1;
     }
     CUtensorMap map;
-    if (!tc_make_map(&map, a.x, a.rows, a.w.K, a.ldx, GM_ROWS)) return cudaErrorInvalidValue;
+    if (!tc_make_map(&map, a.x, a.rows, a.w.K, a.ldx, GM_HALF)) return cudaErrorInvalidValue;
     return x_dtype == BLS_BF16 ? launch_tiles<__nv_bfloat16>(map, a, s) : launch_tiles<__half>(map, a, s);
 }

@@ -595,3 +595,26 @@ def test_places_past_the_rows_are_left_out():
     dw = torch.empty(n, k, device="cuda")
     bls.bls_moe_combine_grad(x, xs, place, offsets, None, torch.empty_like(xs), dw)
     assert torch.all(dw[~kept] == 0)
+
+
+@pytest.mark.parametrize("rows,N,K,group,symmetric,dtype", [
+    (300, 25000, 264, 64, False, BF16), (513, 20000, 130, 32, True, F16), (1000, 12800, 128, 128, True, BF16), (256, 38000, 96, 32, False, BF16),
+])
+def test_linear_of_many_outputs(rows, N, K, group, symmetric, dtype):
+    """Enough tiles for those of 256 rows: whole ones, and ends inside the first and the second half."""
+    g = gen(rows, N, K)
+    t, w = weights(g, 1, N, K, group, symmetric)
+    x = torch.randn(rows, K, device="cuda", generator=g).to(dtype)
+    check_linear(t, w, x, None, torch.randn(1, N, device="cuda", generator=g), 1, dtype)
+
+
+def test_linear_by_experts_of_many_rows():
+    counts = [0, 1000, 1, 0, 127, 129, 257, 0, 2000, 640, 500, 384, 0]
+    E, N, K = len(counts), 1700, 200
+    g = gen("many rows")
+    t, w = weights(g, E, N, K, 64, False)
+    offsets = torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32, device="cuda")
+    x = torch.randn(sum(counts) + 70, K, device="cuda", generator=g).to(BF16)
+    bias = torch.randn(E, N, device="cuda", generator=g)
+    check_linear(t, w, x, offsets, bias, 0, BF16)
+    check_linear(t, w, x, offsets, bias, 2, F32)
