@@ -38,91 +38,182 @@ __device__ __forceinline__ uint4 load_x8(const W4Args &a, long long row, int k)
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// grid (ceil(N / 16), E + 1): 16 outputs of one matrix; the last layer of blocks clears the rows
-// that belong to no matrix.
-template <class T, int NT>
-__global__ void __launch_bounds__(MV_WARPS * 32) bls_w4_rows_kernel(W4Args a)
+// The scales of two outputs and of all groups of a tile: one word per lane (lanes 8 g .. 8 g + 7: group g, outputs
+// 2 (lane mod 8) and the next one of the 16), taken apart by shuffles when they are needed.
+template <int GROUP> struct RowsSide { unsigned scale, zero; };
+
+// Adds the products of up to 8 * NT rows of x with 16 * MT outputs over the tiles warp, warp + MV_WARPS, ..
+// of 128 inputs.  A thread asks for the weights of U tiles before it uses the first.
+template <class T, int GROUP, int MT, int NT, int U>
+__device__ __forceinline__ void rows_product(const W4Args &a, const uint8_t *q, size_t side, int warp, int lane, int base, int hi,
+                                             float (&tot)[MT][NT][4])
 {
-    stream_order_enter();
-    __shared__ float part[MV_WARPS][16][8 * NT];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
-    const int n0 = blockIdx.x * 16, e = blockIdx.y;
+    constexpr int GPT = W4_TILE / GROUP;
     const W4Weights &w = a.w;
-    if (e == w.E) {
-        if (!a.offsets) return;
-        const int first = min(max(a.offsets[w.E], 0), a.rows);
-        for (long long i = threadIdx.x; i < (long long)(a.rows - first) * 16; i += blockDim.x) {
-            const int n = n0 + (int)(i & 15);
-            if (n < w.N) w4_store(a.y, (size_t)(first + (i >> 4)) * a.ldy + n, a.y_dtype, 0.f);
-        }
-        return;
-    }
-    int lo, hi;
-    w4_rows(a, e, lo, hi);
-    const int r0 = n0 % W4_TILE + gid;                                   // this lane's outputs in the tile: r0, r0 + 8
-    const int groups = w.KT * W4_TILE / w.group, gpt = W4_TILE / w.group;
-    const uint8_t *q = w.q + ((size_t)e * w.NT + n0 / W4_TILE) * w.KT * W4_TILE_BYTES + r0 * 64;
-    const int p0 = (tig ^ ((r0 >> 1) & 3)) * 16, p1 = 512 + (tig ^ (((r0 + 8) >> 1) & 3)) * 16;
-    const size_t s0 = (size_t)e * groups * w.NT * W4_TILE + n0 + gid;
-    for (int base = lo; base < hi; base += 8 * NT) {
-        float tot[NT][4], acc[NT][4];
+    const int gid = lane >> 2, tig = lane & 3, KT = w.KT;
+    const size_t np = (size_t)w.NT * W4_TILE;
+    // a lane's piece of output gid (and gid + 8, 512 bytes on, where the same swizzle holds): 64 bytes per output
+    const uint8_t *mine = q + gid * 64 + ((tig ^ ((gid >> 1) & 3)) * 16);
+    const unsigned *scale = (const unsigned *)(w.scale + side + (size_t)(lane >> 3) * np + (lane & 7) * 2);
+    const unsigned short *zero = (const unsigned short *)(w.zero + side + (size_t)(lane >> 3) * np + (lane & 7) * 2);
+    const bool holds = lane < 8 * GPT;
+    for (int kt0 = warp; kt0 < KT; kt0 += MV_WARPS * U) {
+        uint4 qw[U][MT][2];
+        RowsSide<GROUP> sd[U][MT];
         #pragma unroll
-        for (int j = 0; j < NT; j++)
+        for (int u = 0; u < U; u++) {
+            const int kt = kt0 + u * MV_WARPS;
             #pragma unroll
-            for (int c = 0; c < 4; c++) tot[j][c] = acc[j][c] = 0.f;
-        for (int kt = warp; kt < w.KT; kt += MV_WARPS) {
-            const uint4 qa = *(const uint4 *)(q + (size_t)kt * W4_TILE_BYTES + p0);
-            const uint4 qb = *(const uint4 *)(q + (size_t)kt * W4_TILE_BYTES + p1);
-            const unsigned wa[4] = {qa.x, qa.y, qa.z, qa.w}, wb[4] = {qb.x, qb.y, qb.z, qb.w};
-            #pragma unroll
-            for (int b = 0; b < 4; b++) {
-                const int g = kt * gpt + b * 32 / w.group;
-                const size_t sg = s0 + (size_t)g * w.NT * W4_TILE;
-                const unsigned z0 = w4_zero_pair<T>(w.zero ? w.zero[sg] & 15 : 8), z1 = w4_zero_pair<T>(w.zero ? w.zero[sg + 8] & 15 : 8);
-                unsigned pa[4], pb[4];
-                w4_unpack<T>(wa[b], z0, pa);
-                w4_unpack<T>(wb[b], z1, pb);
-                const unsigned f0[4] = {pa[0], pb[0], pa[1], pb[1]}, f1[4] = {pa[2], pb[2], pa[3], pb[3]};
-                #pragma unroll
-                for (int j = 0; j < NT; j++) {
-                    const int row = base + j * 8 + gid;
-                    uint4 x = make_uint4(0, 0, 0, 0);
-                    if (row < hi) x = load_x8<T>(a, row, kt * W4_TILE + b * 32 + tig * 8);
-                    mma_16816(acc[j], f0, x.x, x.y, T());
-                    mma_16816(acc[j], f1, x.z, x.w, T());
-                }
-                if ((b + 1) * 32 % w.group == 0) {                        // the group's sum is complete: scale it
-                    const float sc0 = __bfloat162float(w.scale[sg]), sc1 = __bfloat162float(w.scale[sg + 8]);
-                    #pragma unroll
-                    for (int j = 0; j < NT; j++) {
-                        tot[j][0] = fmaf(sc0, acc[j][0], tot[j][0]);
-                        tot[j][1] = fmaf(sc0, acc[j][1], tot[j][1]);
-                        tot[j][2] = fmaf(sc1, acc[j][2], tot[j][2]);
-                        tot[j][3] = fmaf(sc1, acc[j][3], tot[j][3]);
-                        #pragma unroll
-                        for (int c = 0; c < 4; c++) acc[j][c] = 0.f;
+            for (int m = 0; m < MT; m++) {
+                qw[u][m][0] = qw[u][m][1] = make_uint4(0, 0, 0, 0);
+                sd[u][m].scale = 0; sd[u][m].zero = 0x0808;
+                if (kt < KT) {
+                    const uint8_t *p = mine + (size_t)kt * W4_TILE_BYTES + m * 1024;
+                    qw[u][m][0] = __ldcs((const uint4 *)p);                        // read once: nothing else has to leave L2 for it
+                    qw[u][m][1] = __ldcs((const uint4 *)(p + 512));
+                    if (holds) {
+                        sd[u][m].scale = __ldg(scale + ((size_t)kt * GPT * np + m * 16) / 2);
+                        if (w.zero) sd[u][m].zero = __ldg(zero + ((size_t)kt * GPT * np + m * 16) / 2);
                     }
                 }
             }
         }
-        __syncthreads();                                                  // the previous chunk's sums have been read
         #pragma unroll
-        for (int j = 0; j < NT; j++) {
-            part[warp][gid][j * 8 + tig * 2] = tot[j][0];
-            part[warp][gid][j * 8 + tig * 2 + 1] = tot[j][1];
-            part[warp][gid + 8][j * 8 + tig * 2] = tot[j][2];
-            part[warp][gid + 8][j * 8 + tig * 2 + 1] = tot[j][3];
+        for (int u = 0; u < U; u++) {
+            const int kt = kt0 + u * MV_WARPS;
+            if (kt >= KT) break;
+            float acc[MT][NT][4];
+            #pragma unroll
+            for (int b = 0; b < 4; b++) {
+                if (b * 32 % GROUP == 0) {
+                    #pragma unroll
+                    for (int m = 0; m < MT; m++)
+                        #pragma unroll
+                        for (int j = 0; j < NT; j++)
+                            #pragma unroll
+                            for (int c = 0; c < 4; c++) acc[m][j][c] = 0.f;
+                }
+                uint4 x[NT];
+                #pragma unroll
+                for (int j = 0; j < NT; j++) {
+                    const int row = base + j * 8 + gid;
+                    x[j] = make_uint4(0, 0, 0, 0);
+                    if (row < hi) x[j] = load_x8<T>(a, row, kt * W4_TILE + b * 32 + tig * 8);
+                }
+                const int from = b * 32 / GROUP * 8 + (gid >> 1);
+                #pragma unroll
+                for (int m = 0; m < MT; m++) {
+                    const unsigned za = __shfl_sync(~0u, sd[u][m].zero, from), zb = __shfl_sync(~0u, sd[u][m].zero, from + 4);
+                    const unsigned z0 = w4_zero_pair<T>(za >> (8 * (gid & 1)) & 15), z1 = w4_zero_pair<T>(zb >> (8 * (gid & 1)) & 15);
+                    const unsigned wa = b == 0 ? qw[u][m][0].x : b == 1 ? qw[u][m][0].y : b == 2 ? qw[u][m][0].z : qw[u][m][0].w;
+                    const unsigned wb = b == 0 ? qw[u][m][1].x : b == 1 ? qw[u][m][1].y : b == 2 ? qw[u][m][1].z : qw[u][m][1].w;
+                    unsigned pa[4], pb[4];
+                    w4_unpack<T>(wa, z0, pa);
+                    w4_unpack<T>(wb, z1, pb);
+                    const unsigned f0[4] = {pa[0], pb[0], pa[1], pb[1]}, f1[4] = {pa[2], pb[2], pa[3], pb[3]};
+                    #pragma unroll
+                    for (int j = 0; j < NT; j++) {
+                        mma_16816(acc[m][j], f0, x[j].x, x[j].y, T());
+                        mma_16816(acc[m][j], f1, x[j].z, x[j].w, T());
+                    }
+                    if ((b + 1) * 32 % GROUP == 0) {                              // the group's sum is complete: scale it
+                        const unsigned sa = __shfl_sync(~0u, sd[u][m].scale, from), sb = __shfl_sync(~0u, sd[u][m].scale, from + 4);
+                        const float s0 = __uint_as_float(gid & 1 ? sa & 0xffff0000u : sa << 16), s1 = __uint_as_float(gid & 1 ? sb & 0xffff0000u : sb << 16);
+                        #pragma unroll
+                        for (int j = 0; j < NT; j++) {
+                            tot[m][j][0] = fmaf(s0, acc[m][j][0], tot[m][j][0]);
+                            tot[m][j][1] = fmaf(s0, acc[m][j][1], tot[m][j][1]);
+                            tot[m][j][2] = fmaf(s1, acc[m][j][2], tot[m][j][2]);
+                            tot[m][j][3] = fmaf(s1, acc[m][j][3], tot[m][j][3]);
+                        }
+                    }
+                }
+            }
+        }
+    }
+}
+
+// 8 * NT rows of x from `base` on: the warps' parts of the sums meet in shared memory, in the order of the warps.
+template <class T, int GROUP, int MT, int NT>
+__device__ __forceinline__ void rows_chunk(const W4Args &a, const uint8_t *q, size_t side, int e, int n0, int base, int hi, float *part)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+    constexpr int O = 16 * MT, R = 8 * NT;
+    float tot[MT][NT][4];
+    #pragma unroll
+    for (int m = 0; m < MT; m++)
+        #pragma unroll
+        for (int j = 0; j < NT; j++)
+            #pragma unroll
+            for (int c = 0; c < 4; c++) tot[m][j][c] = 0.f;
+    rows_product<T, GROUP, MT, NT, 2>(a, q, side, warp, lane, base, hi, tot);
+    __syncthreads();                                                      // the previous chunk's sums have been read
+    float *mine = part + warp * O * R;
+    #pragma unroll
+    for (int m = 0; m < MT; m++)
+        #pragma unroll
+        for (int j = 0; j < NT; j++)
+            #pragma unroll
+            for (int c = 0; c < 4; c++) mine[(j * 8 + tig * 2 + (c & 1)) * O + m * 16 + gid + (c >> 1) * 8] = tot[m][j][c];
+    __syncthreads();
+    for (int i = threadIdx.x; i < O * R; i += MV_WARPS * 32) {
+        const int n = n0 + i % O, row = base + i / O;
+        if (n >= a.w.N || row >= hi) continue;
+        float v = 0.f;
+        #pragma unroll
+        for (int k = 0; k < MV_WARPS; k++) v += part[k * O * R + i];
+        if (a.bias) v += a.bias[(size_t)e * a.w.N + n];
+        w4_store(a.y, (size_t)row * a.ldy + n, a.y_dtype, w4_act(v, a.act));
+    }
+}
+
+// grid (ceil(N / (16 MT)), min(E, rows), + 1 with offsets): 16 MT outputs of one matrix that has rows; with fewer rows
+// than matrices the y-th one that has any.  The last layer of blocks clears the rows that belong to no matrix.
+template <class T, int GROUP, int MT, int NT>
+__global__ void __launch_bounds__(MV_WARPS * 32) bls_w4_rows_kernel(const __grid_constant__ W4Args a)
+{
+    stream_order_enter();
+    __shared__ float part[MV_WARPS * 16 * MT * 8 * NT];
+    __shared__ int found;
+    const int n0 = blockIdx.x * 16 * MT;
+    const W4Weights &w = a.w;
+    const int layers = min(w.E, a.rows);
+    int e = blockIdx.y;
+    if (e == layers) {
+        const int first = min(max(a.offsets[w.E], 0), a.rows);
+        for (long long i = threadIdx.x; i < (long long)(a.rows - first) * 16 * MT; i += blockDim.x) {
+            const int n = n0 + (int)(i % (16 * MT));
+            if (n < w.N) w4_store(a.y, (size_t)(first + i / (16 * MT)) * a.ldy + n, a.y_dtype, 0.f);
+        }
+        return;
+    }
+    if (a.offsets && layers < w.E) {
+        // the matrices that have rows are counted by the first warp, 32 at a time
+        if (threadIdx.x < 32) {
+            int seen = 0, at = -1;
+            for (int e0 = 0; e0 < w.E && at < 0; e0 += 32) {
+                int lo = 0, hi = 0;
+                if (e0 + (int)threadIdx.x < w.E) w4_rows(a, e0 + threadIdx.x, lo, hi);
+                unsigned some = __ballot_sync(~0u, hi > lo);
+                const int c = __popc(some);
+                if (seen + c > e) at = e0 + __fns(some, 0, e - seen + 1);
+                seen += c;
+            }
+            if (threadIdx.x == 0) found = at;
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < 16 * 8 * NT; i += blockDim.x) {
-            const int o = i & 15, r = i >> 4, n = n0 + o, row = base + r;
-            if (n >= w.N || row >= hi) continue;
-            float v = 0.f;
-            #pragma unroll
-            for (int k = 0; k < MV_WARPS; k++) v += part[k][o][r];
-            if (a.bias) v += a.bias[(size_t)e * w.N + n];
-            w4_store(a.y, (size_t)row * a.ldy + n, a.y_dtype, w4_act(v, a.act));
-        }
+        e = found;
+        if (e < 0) return;
+    }
+    int lo, hi;
+    w4_rows(a, e, lo, hi);
+    const uint8_t *q = w.q + ((size_t)e * w.NT + n0 / W4_TILE) * w.KT * W4_TILE_BYTES + n0 % W4_TILE * 64;
+    const size_t side = (size_t)e * (w.KT * (W4_TILE / GROUP)) * w.NT * W4_TILE + n0;
+    for (int base = lo; base < hi; ) {
+        const int left = hi - base;
+        if (NT >= 4 && left > 16) { rows_chunk<T, GROUP, MT, NT >= 4 ? 4 : 1>(a, q, side, e, n0, base, hi, part); base += 32; }
+        else if (NT >= 2 && left > 8) { rows_chunk<T, GROUP, MT, NT >= 2 ? 2 : 1>(a, q, side, e, n0, base, hi, part); base += 16; }
+        else { rows_chunk<T, GROUP, MT, 1>(a, q, side, e, n0, base, hi, part); base += 8; }
     }
 }
 
@@ -338,17 +429,24 @@ bool w4_shape(int E, int N, int K, int group, W4Weights &w)
 // Which kernel: by the rows that a matrix gets on average.
 bool many_rows(const W4Weights &w, int64_t rows) { return rows > 32ll * w.E; }
 
-template <class T, int NT>
-cudaError_t launch_rows(const W4Args &a, cudaStream_t s)
+template <class T, int GROUP, int MT>
+cudaError_t launch_rows_m(const W4Args &a, cudaStream_t s)
 {
-    return launch_serialised(bls_w4_rows_kernel<T, NT>, dim3((a.w.N + 15) / 16, a.w.E + (a.offsets ? 1 : 0)), dim3(MV_WARPS * 32), s, a);
+    const dim3 grid((a.w.N + 16 * MT - 1) / (16 * MT), min(a.w.E, a.rows) + (a.offsets ? 1 : 0)), block(MV_WARPS * 32);
+    return a.rows <= 8 ? launch_serialised(bls_w4_rows_kernel<T, GROUP, MT, 1>, grid, block, s, a) :
+           a.rows <= 16 ? launch_serialised(bls_w4_rows_kernel<T, GROUP, MT, 2>, grid, block, s, a) :
+                          launch_serialised(bls_w4_rows_kernel<T, GROUP, MT, 4>, grid, block, s, a);
+}
+template <class T, int GROUP>
+cudaError_t launch_rows_g(const W4Args &a, cudaStream_t s)
+{
+    const long long blocks = (long long)((a.w.N + 31) / 32) * min(a.w.E, a.rows);
+    return blocks >= 2 * 148 ? launch_rows_m<T, GROUP, 2>(a, s) : launch_rows_m<T, GROUP, 1>(a, s);
 }
 template <class T>
-cudaError_t launch_linear4(const W4Args &a, cudaStream_t s)
+cudaError_t launch_rows(const W4Args &a, cudaStream_t s)
 {
-    if (a.rows <= 8) return launch_rows<T, 1>(a, s);
-    if (a.rows <= 16) return launch_rows<T, 2>(a, s);
-    return launch_rows<T, 4>(a, s);
+    return a.w.group == 32 ? launch_rows_g<T, 32>(a, s) : a.w.group == 64 ? launch_rows_g<T, 64>(a, s) : launch_rows_g<T, 128>(a, s);
 }
 
 }  // namespace
@@ -413,7 +511,7 @@ bls_status_t bls_w4_linear(const uint8_t *q, const void *scale, const uint8_t *z
     a.x = x; a.ldx = ldx; a.rows = (int)rows; a.x_pieces = ((uintptr_t)x & 15) == 0 && ldx % 8 == 0;
     a.offsets = offsets; a.bias = bias; a.act = act; a.y = y; a.y_dtype = y_dtype; a.ldy = ldy; a.status = status;
     cudaError_t r = many_rows(a.w, rows) ? w4_tiles(a, x_dtype, workspace, (cudaStream_t)cuda_stream) :
-                    x_dtype == BLS_BF16 ? launch_linear4<__nv_bfloat16>(a, (cudaStream_t)cuda_stream) : launch_linear4<__half>(a, (cudaStream_t)cuda_stream);
+                    x_dtype == BLS_BF16 ? launch_rows<__nv_bfloat16>(a, (cudaStream_t)cuda_stream) : launch_rows<__half>(a, (cudaStream_t)cuda_stream);
     return r == cudaSuccess ? BLS_OK : BLS_ECUDA;
 }
 
