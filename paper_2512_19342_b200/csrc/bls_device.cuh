@@ -24,20 +24,30 @@ __device__ __forceinline__ void stream_order_enter()
 }
 
 template <class... Params, class... Args>
-static inline cudaError_t launch_serialised_smem(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem,
-                                                 cudaStream_t stream, Args... args)
+static inline cudaError_t launch_serialised_cluster(void (*kernel)(Params...), dim3 grid, dim3 block, int cluster, size_t smem,
+                                                    cudaStream_t stream, Args... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
+}
+
+template <class... Params, class... Args>
+static inline cudaError_t launch_serialised_smem(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem,
+                                                 cudaStream_t stream, Args... args)
+{
+    return launch_serialised_cluster(kernel, grid, block, 1, smem, stream, args...);
 }
 
 template <class... Params, class... Args>

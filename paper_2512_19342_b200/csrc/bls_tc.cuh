@@ -22,6 +22,10 @@ __device__ __forceinline__ void mb_expect_tx(unsigned bar, unsigned bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void mb_arrive(unsigned bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 // Bounded wait for the phase with the given parity: false (and the status bit) after two seconds.
 __device__ __forceinline__ bool mb_wait(unsigned bar, unsigned parity, int *status)
 {
@@ -45,6 +49,11 @@ __device__ __forceinline__ void tma_load_2d(unsigned dst, const CUtensorMap *map
 {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                  ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void bulk_load(unsigned dst, const void *src, unsigned bytes, unsigned bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 // Shared-memory matrix descriptor of a K-major tile stored with the 128-byte swizzle:
 // rows of 128 bytes, groups of 8 rows 1024 bytes apart (stride byte offset), descriptor

@@ -6,27 +6,41 @@
 // row).  The weights are the A operand of mma.m16n8k16 (16 outputs x 16 inputs), 8 rows of x the
 // B operand: an instruction then takes 256 weights for one word per lane, which leaves the ALUs
 // only the unpacking.  The order of the inputs inside a product is free, so a lane
-// takes the inputs that one stored 16-byte piece holds, and reads the same 8 neighbouring x values per word.
+// takes the inputs that one stored 16-byte piece holds, and the same 8 neighbouring x values per word.
+//
+// At this size a layer is a few such steps per warp, so what counts is that all loads are on their way
+// at once and that many warps share the unpacking: the 16 warps of a block split K (and, where K is short
+// or there is plenty of work, also the outputs), and their sums meet in shared memory in the order of the slices.
 #include "bls_w4.cuh"
 #include "bls_w4_gemm.h"
 
 namespace {
 
-constexpr int MV_WARPS = 8;                  // the warps of a block share 16 outputs and split K
+constexpr int FR_WARPS = 16;
+constexpr int FR_U = 2;                              // tiles of weights a warp has on their way
 
-__device__ __forceinline__ void mma_16816(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1, __nv_bfloat16)
+__device__ __forceinline__ void mma_16816(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1, bool first, __nv_bfloat16)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    if (first) {                                     // known when compiled: c = a b
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+        return;
+    }
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma_16816(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1, __half)
+__device__ __forceinline__ void mma_16816(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1, bool first, __half)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    if (first) {                                     // known when compiled: c = a b
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+        return;
+    }
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Eight x values from input k on, zeros past K.
-template <class T>
+// Eight x values of a row from input k on, zeros past K.
 __device__ __forceinline__ uint4 load_x8(const W4Args &a, long long row, int k)
 {
     const unsigned short *p = (const unsigned short *)a.x + row * a.ldx + k;
@@ -38,152 +52,26 @@ __device__ __forceinline__ uint4 load_x8(const W4Args &a, long long row, int k)
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// The scales of two outputs and of all groups of a tile: one word per lane (lanes 8 g .. 8 g + 7: group g, outputs
-// 2 (lane mod 8) and the next one of the 16), taken apart by shuffles when they are needed.
-template <int GROUP> struct RowsSide { unsigned scale, zero; };
-
-// Adds the products of up to 8 * NT rows of x with 16 * MT outputs over the tiles warp, warp + MV_WARPS, ..
-// of 128 inputs.  A thread asks for the weights of U tiles before it uses the first.
-template <class T, int GROUP, int MT, int NT, int U>
-__device__ __forceinline__ void rows_product(const W4Args &a, const uint8_t *q, size_t side, int warp, int lane, int base, int hi,
-                                             float (&tot)[MT][NT][4])
-{
-    constexpr int GPT = W4_TILE / GROUP;
-    const W4Weights &w = a.w;
-    const int gid = lane >> 2, tig = lane & 3, KT = w.KT;
-    const size_t np = (size_t)w.NT * W4_TILE;
-    // a lane's piece of output gid (and gid + 8, 512 bytes on, where the same swizzle holds): 64 bytes per output
-    const uint8_t *mine = q + gid * 64 + ((tig ^ ((gid >> 1) & 3)) * 16);
-    const unsigned *scale = (const unsigned *)(w.scale + side + (size_t)(lane >> 3) * np + (lane & 7) * 2);
-    const unsigned short *zero = (const unsigned short *)(w.zero + side + (size_t)(lane >> 3) * np + (lane & 7) * 2);
-    const bool holds = lane < 8 * GPT;
-    for (int kt0 = warp; kt0 < KT; kt0 += MV_WARPS * U) {
-        uint4 qw[U][MT][2];
-        RowsSide<GROUP> sd[U][MT];
-        #pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int kt = kt0 + u * MV_WARPS;
-            #pragma unroll
-            for (int m = 0; m < MT; m++) {
-                qw[u][m][0] = qw[u][m][1] = make_uint4(0, 0, 0, 0);
-                sd[u][m].scale = 0; sd[u][m].zero = 0x0808;
-                if (kt < KT) {
-                    const uint8_t *p = mine + (size_t)kt * W4_TILE_BYTES + m * 1024;
-                    qw[u][m][0] = __ldcs((const uint4 *)p);                        // read once: nothing else has to leave L2 for it
-                    qw[u][m][1] = __ldcs((const uint4 *)(p + 512));
-                    if (holds) {
-                        sd[u][m].scale = __ldg(scale + ((size_t)kt * GPT * np + m * 16) / 2);
-                        if (w.zero) sd[u][m].zero = __ldg(zero + ((size_t)kt * GPT * np + m * 16) / 2);
-                    }
-                }
-            }
-        }
-        #pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int kt = kt0 + u * MV_WARPS;
-            if (kt >= KT) break;
-            float acc[MT][NT][4];
-            #pragma unroll
-            for (int b = 0; b < 4; b++) {
-                if (b * 32 % GROUP == 0) {
-                    #pragma unroll
-                    for (int m = 0; m < MT; m++)
-                        #pragma unroll
-                        for (int j = 0; j < NT; j++)
-                            #pragma unroll
-                            for (int c = 0; c < 4; c++) acc[m][j][c] = 0.f;
-                }
-                uint4 x[NT];
-                #pragma unroll
-                for (int j = 0; j < NT; j++) {
-                    const int row = base + j * 8 + gid;
-                    x[j] = make_uint4(0, 0, 0, 0);
-                    if (row < hi) x[j] = load_x8<T>(a, row, kt * W4_TILE + b * 32 + tig * 8);
-                }
-                const int from = b * 32 / GROUP * 8 + (gid >> 1);
-                #pragma unroll
-                for (int m = 0; m < MT; m++) {
-                    const unsigned za = __shfl_sync(~0u, sd[u][m].zero, from), zb = __shfl_sync(~0u, sd[u][m].zero, from + 4);
-                    const unsigned z0 = w4_zero_pair<T>(za >> (8 * (gid & 1)) & 15), z1 = w4_zero_pair<T>(zb >> (8 * (gid & 1)) & 15);
-                    const unsigned wa = b == 0 ? qw[u][m][0].x : b == 1 ? qw[u][m][0].y : b == 2 ? qw[u][m][0].z : qw[u][m][0].w;
-                    const unsigned wb = b == 0 ? qw[u][m][1].x : b == 1 ? qw[u][m][1].y : b == 2 ? qw[u][m][1].z : qw[u][m][1].w;
-                    unsigned pa[4], pb[4];
-                    w4_unpack<T>(wa, z0, pa);
-                    w4_unpack<T>(wb, z1, pb);
-                    const unsigned f0[4] = {pa[0], pb[0], pa[1], pb[1]}, f1[4] = {pa[2], pb[2], pa[3], pb[3]};
-                    #pragma unroll
-                    for (int j = 0; j < NT; j++) {
-                        mma_16816(acc[m][j], f0, x[j].x, x[j].y, T());
-                        mma_16816(acc[m][j], f1, x[j].z, x[j].w, T());
-                    }
-                    if ((b + 1) * 32 % GROUP == 0) {                              // the group's sum is complete: scale it
-                        const unsigned sa = __shfl_sync(~0u, sd[u][m].scale, from), sb = __shfl_sync(~0u, sd[u][m].scale, from + 4);
-                        const float s0 = __uint_as_float(gid & 1 ? sa & 0xffff0000u : sa << 16), s1 = __uint_as_float(gid & 1 ? sb & 0xffff0000u : sb << 16);
-                        #pragma unroll
-                        for (int j = 0; j < NT; j++) {
-                            tot[m][j][0] = fmaf(s0, acc[m][j][0], tot[m][j][0]);
-                            tot[m][j][1] = fmaf(s0, acc[m][j][1], tot[m][j][1]);
-                            tot[m][j][2] = fmaf(s1, acc[m][j][2], tot[m][j][2]);
-                            tot[m][j][3] = fmaf(s1, acc[m][j][3], tot[m][j][3]);
-                        }
-                    }
-                }
-            }
-        }
-    }
-}
-
-// 8 * NT rows of x from `base` on: the warps' parts of the sums meet in shared memory, in the order of the warps.
-template <class T, int GROUP, int MT, int NT>
-__device__ __forceinline__ void rows_chunk(const W4Args &a, const uint8_t *q, size_t side, int e, int n0, int base, int hi, float *part)
-{
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
-    constexpr int O = 16 * MT, R = 8 * NT;
-    float tot[MT][NT][4];
-    #pragma unroll
-    for (int m = 0; m < MT; m++)
-        #pragma unroll
-        for (int j = 0; j < NT; j++)
-            #pragma unroll
-            for (int c = 0; c < 4; c++) tot[m][j][c] = 0.f;
-    rows_product<T, GROUP, MT, NT, 2>(a, q, side, warp, lane, base, hi, tot);
-    __syncthreads();                                                      // the previous chunk's sums have been read
-    float *mine = part + warp * O * R;
-    #pragma unroll
-    for (int m = 0; m < MT; m++)
-        #pragma unroll
-        for (int j = 0; j < NT; j++)
-            #pragma unroll
-            for (int c = 0; c < 4; c++) mine[(j * 8 + tig * 2 + (c & 1)) * O + m * 16 + gid + (c >> 1) * 8] = tot[m][j][c];
-    __syncthreads();
-    for (int i = threadIdx.x; i < O * R; i += MV_WARPS * 32) {
-        const int n = n0 + i % O, row = base + i / O;
-        if (n >= a.w.N || row >= hi) continue;
-        float v = 0.f;
-        #pragma unroll
-        for (int k = 0; k < MV_WARPS; k++) v += part[k * O * R + i];
-        if (a.bias) v += a.bias[(size_t)e * a.w.N + n];
-        w4_store(a.y, (size_t)row * a.ldy + n, a.y_dtype, w4_act(v, a.act));
-    }
-}
-
-// grid (ceil(N / (16 MT)), min(E, rows), + 1 with offsets): 16 MT outputs of one matrix that has rows; with fewer rows
-// than matrices the y-th one that has any.  The last layer of blocks clears the rows that belong to no matrix.
-template <class T, int GROUP, int MT, int NT>
-__global__ void __launch_bounds__(MV_WARPS * 32) bls_w4_rows_kernel(const __grid_constant__ W4Args a)
+// grid (blocks of 16 * OW outputs, min(E, rows), + 1 with offsets), OW = 16 >> kw_log: the outputs of one matrix that
+// has rows; with fewer rows than matrices the y-th one that has any.  KW = 1 << kw_log warps split K.
+// The last layer of blocks clears the rows that belong to no matrix.
+template <class T, int GROUP, bool ZERO>
+__global__ void __launch_bounds__(FR_WARPS * 32, 2) bls_w4_rows_kernel(const __grid_constant__ W4Args a, int kw_log)
 {
     stream_order_enter();
-    __shared__ float part[MV_WARPS * 16 * MT * 8 * NT];
+    constexpr int GPT = W4_TILE / GROUP;
+    extern __shared__ __align__(16) unsigned char fr_smem[];
     __shared__ int found;
-    const int n0 = blockIdx.x * 16 * MT;
     const W4Weights &w = a.w;
+    const int KW = 1 << kw_log, outs = 16 * (FR_WARPS >> kw_log);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
     const int layers = min(w.E, a.rows);
     int e = blockIdx.y;
     if (e == layers) {
         const int first = min(max(a.offsets[w.E], 0), a.rows);
-        for (long long i = threadIdx.x; i < (long long)(a.rows - first) * 16 * MT; i += blockDim.x) {
-            const int n = n0 + (int)(i % (16 * MT));
-            if (n < w.N) w4_store(a.y, (size_t)(first + i / (16 * MT)) * a.ldy + n, a.y_dtype, 0.f);
+        for (long long i = threadIdx.x; i < (long long)(a.rows - first) * outs; i += blockDim.x) {
+            const int n = blockIdx.x * outs + (int)(i % outs);
+            if (n < w.N) w4_store(a.y, (size_t)(first + i / outs) * a.ldy + n, a.y_dtype, 0.f);
         }
         return;
     }
@@ -207,13 +95,94 @@ __global__ void __launch_bounds__(MV_WARPS * 32) bls_w4_rows_kernel(const __grid
     }
     int lo, hi;
     w4_rows(a, e, lo, hi);
-    const uint8_t *q = w.q + ((size_t)e * w.NT + n0 / W4_TILE) * w.KT * W4_TILE_BYTES + n0 % W4_TILE * 64;
-    const size_t side = (size_t)e * (w.KT * (W4_TILE / GROUP)) * w.NT * W4_TILE + n0;
-    for (int base = lo; base < hi; ) {
-        const int left = hi - base;
-        if (NT >= 4 && left > 16) { rows_chunk<T, GROUP, MT, NT >= 4 ? 4 : 1>(a, q, side, e, n0, base, hi, part); base += 32; }
-        else if (NT >= 2 && left > 8) { rows_chunk<T, GROUP, MT, NT >= 2 ? 2 : 1>(a, q, side, e, n0, base, hi, part); base += 16; }
-        else { rows_chunk<T, GROUP, MT, 1>(a, q, side, e, n0, base, hi, part); base += 8; }
+    const int kw = warp & (KW - 1), n0 = blockIdx.x * outs + (warp >> kw_log) * 16, KT = w.KT;
+    const bool live = n0 < w.N;
+    // a lane's piece of output gid (and gid + 8, 512 bytes on, where the same swizzle holds): 64 bytes per output
+    const uint8_t *q = w.q + ((size_t)e * w.NT + n0 / W4_TILE) * KT * W4_TILE_BYTES + (n0 % W4_TILE + gid) * 64 + ((tig ^ ((gid >> 1) & 3)) * 16);
+    // scales and zero points of a tile are held by lanes 8 g .. 8 g + 7 (and the lanes 8 GPT on): group g, outputs
+    // 2 (lane mod 8) and the next one
+    const size_t np = (size_t)w.NT * W4_TILE, side = (size_t)e * KT * GPT * np + n0 + (size_t)(lane >> 3 & (GPT - 1)) * np + (lane & 7) * 2;
+    const int round = KW * FR_U, pitch = round * W4_TILE * 2 + 64;            // 64 past a multiple of 128: two rows fill the banks
+    const int pieces_log = kw_log + 5;                                        // 16-byte pieces of a row in a round: KW * 2 * 16
+    const size_t gstep = (size_t)KW * GPT * np;                               // scales from a tile to this warp's next one
+    const int piece = threadIdx.x & ((1 << pieces_log) - 1), row0 = threadIdx.x >> pieces_log;
+    for (int base = lo; base < hi; base += 8) {
+        const int cnt = min(8, hi - base);
+        float tot[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint8_t *qk = q + (size_t)kw * W4_TILE_BYTES;
+        const __nv_bfloat16 *sk = w.scale + side + (size_t)(kw * GPT) * np;
+        const uint8_t *zk = w.zero + side + (size_t)(kw * GPT) * np;
+        for (int k0 = 0; k0 < KT; k0 += round) {
+            const int mine = live ? KT - k0 - kw : 0;                         // > u * KW: this warp has tile u of the round
+            uint4 qw[FR_U][2];
+            unsigned sc[FR_U], zr[FR_U];
+            #pragma unroll
+            for (int u = 0; u < FR_U; u++) {
+                sc[u] = 0; zr[u] = 0x0808;
+                if (mine > u * KW) {
+                    qw[u][0] = __ldcs((const uint4 *)qk);
+                    qw[u][1] = __ldcs((const uint4 *)(qk + 512));
+                    sc[u] = __ldg((const unsigned *)sk);
+                    if (ZERO) zr[u] = __ldg((const unsigned short *)zk);
+                }
+                qk += KW * W4_TILE_BYTES;
+                sk += gstep;
+                if (ZERO) zk += gstep;
+            }
+            if (k0) __syncthreads();                                          // the previous round's x has been used
+            if (k0 * (W4_TILE / 8) + piece < KT * (W4_TILE / 8))
+                for (int r = row0; r < cnt; r += FR_WARPS * 32 >> pieces_log)
+                    *(uint4 *)(fr_smem + r * pitch + piece * 16) = load_x8(a, base + r, k0 * W4_TILE + piece * 8);
+            __syncthreads();
+            // rows past cnt take the last one's x: a column of the product depends on its own row alone, and theirs are not stored
+            #pragma unroll
+            for (int u = 0; u < FR_U; u++) {
+                if (mine <= u * KW) break;
+                const unsigned char *xs = fr_smem + min(gid, cnt - 1) * pitch + (u * KW + kw) * W4_TILE * 2 + tig * 16;
+                const unsigned wa[4] = {qw[u][0].x, qw[u][0].y, qw[u][0].z, qw[u][0].w}, wb[4] = {qw[u][1].x, qw[u][1].y, qw[u][1].z, qw[u][1].w};
+                float acc[2][4];                                              // two chains of products
+                #pragma unroll
+                for (int b = 0; b < 4; b++) {
+                    const uint4 x = *(const uint4 *)(xs + b * 64);
+                    const int from = b * 32 / GROUP * 8 + (gid >> 1);
+                    unsigned z0 = w4_zero_pair<T>(8), z1 = z0;
+                    if (ZERO) {
+                        z0 = w4_zero_pair<T>(__shfl_sync(~0u, zr[u], from) >> (8 * (gid & 1)) & 15);
+                        z1 = w4_zero_pair<T>(__shfl_sync(~0u, zr[u], from + 4) >> (8 * (gid & 1)) & 15);
+                    }
+                    unsigned pa[4], pb[4];
+                    w4_unpack<T>(wa[b], z0, pa);
+                    w4_unpack<T>(wb[b], z1, pb);
+                    const unsigned f0[4] = {pa[0], pb[0], pa[1], pb[1]}, f1[4] = {pa[2], pb[2], pa[3], pb[3]};
+                    mma_16816(acc[0], f0, x.x, x.y, b * 32 % GROUP == 0, T());
+                    mma_16816(acc[1], f1, x.z, x.w, b * 32 % GROUP == 0, T());
+                    if ((b + 1) * 32 % GROUP == 0) {                          // the group's sum is complete: scale it
+                        const unsigned sa = __shfl_sync(~0u, sc[u], from), sb = __shfl_sync(~0u, sc[u], from + 4);
+                        const float s0 = __uint_as_float(gid & 1 ? sa & 0xffff0000u : sa << 16), s1 = __uint_as_float(gid & 1 ? sb & 0xffff0000u : sb << 16);
+                        tot[0] = fmaf(s0, acc[0][0] + acc[1][0], tot[0]);
+                        tot[1] = fmaf(s0, acc[0][1] + acc[1][1], tot[1]);
+                        tot[2] = fmaf(s1, acc[0][2] + acc[1][2], tot[2]);
+                        tot[3] = fmaf(s1, acc[0][3] + acc[1][3], tot[3]);
+                    }
+                }
+            }
+        }
+        // tot: outputs gid, gid + 8 of rows 2 tig, 2 tig + 1
+        __syncthreads();                                                      // x has been used
+        float *part = (float *)fr_smem;                                       // [KW][8 rows][outs]
+        #pragma unroll
+        for (int c = 0; c < 4; c++) part[(kw * 8 + tig * 2 + (c & 1)) * outs + (warp >> kw_log) * 16 + gid + (c >> 1) * 8] = tot[c];
+        __syncthreads();
+        const int outs_log = 8 - kw_log;
+        for (int i = threadIdx.x; i < cnt << outs_log; i += FR_WARPS * 32) {
+            const int n = blockIdx.x * outs + (i & (outs - 1)), r = i >> outs_log;
+            if (n >= w.N) continue;
+            float v = 0.f;
+            for (int k = 0; k < KW; k++) v += part[(k << (outs_log + 3)) + i];
+            if (a.bias) v += a.bias[(size_t)e * w.N + n];
+            w4_store(a.y, (size_t)(base + r) * a.ldy + n, a.y_dtype, w4_act(v, a.act));
+        }
+        if (base + 8 < hi) __syncthreads();
     }
 }
 
@@ -429,19 +398,19 @@ bool w4_shape(int E, int N, int K, int group, W4Weights &w)
 // Which kernel: by the rows that a matrix gets on average.
 bool many_rows(const W4Weights &w, int64_t rows) { return rows > 32ll * w.E; }
 
-template <class T, int GROUP, int MT>
-cudaError_t launch_rows_m(const W4Args &a, cudaStream_t s)
-{
-    const dim3 grid((a.w.N + 16 * MT - 1) / (16 * MT), min(a.w.E, a.rows) + (a.offsets ? 1 : 0)), block(MV_WARPS * 32);
-    return a.rows <= 8 ? launch_serialised(bls_w4_rows_kernel<T, GROUP, MT, 1>, grid, block, s, a) :
-           a.rows <= 16 ? launch_serialised(bls_w4_rows_kernel<T, GROUP, MT, 2>, grid, block, s, a) :
-                          launch_serialised(bls_w4_rows_kernel<T, GROUP, MT, 4>, grid, block, s, a);
-}
 template <class T, int GROUP>
 cudaError_t launch_rows_g(const W4Args &a, cudaStream_t s)
 {
-    const long long blocks = (long long)((a.w.N + 31) / 32) * min(a.w.E, a.rows);
-    return blocks >= 2 * 148 ? launch_rows_m<T, GROUP, 2>(a, s) : launch_rows_m<T, GROUP, 1>(a, s);
+    const int layers = min(a.w.E, a.rows);
+    // K is split over as many warps as have two tiles each, or fewer where the outputs alone keep 32 warps on every SM busy
+    int kw_log = 4;
+    while (kw_log > 0 && ((a.w.KT < FR_U << kw_log) || (((long long)(a.w.N + 15) / 16 * layers) << kw_log) > 2 * 32 * 148)) kw_log--;
+    const int outs = 16 * (FR_WARPS >> kw_log), rows = min(8, a.rows);
+    const size_t smem = max((size_t)rows * ((FR_U << kw_log) * W4_TILE * 2 + 64), (size_t)FR_WARPS * 16 * 8 * sizeof(float));
+    auto kernel = a.w.zero ? bls_w4_rows_kernel<T, GROUP, true> : bls_w4_rows_kernel<T, GROUP, false>;
+    cudaError_t e = smem <= 48 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    return launch_serialised_smem(kernel, dim3((a.w.N + outs - 1) / outs, layers + (a.offsets ? 1 : 0)), dim3(FR_WARPS * 32), smem, s, a, kw_log);
 }
 template <class T>
 cudaError_t launch_rows(const W4Args &a, cudaStream_t s)

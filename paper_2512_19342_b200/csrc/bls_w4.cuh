@@ -61,26 +61,30 @@ __device__ __forceinline__ void w4_rows(const W4Args &a, int e, int &lo, int &hi
 
 // Four pairs of neighbouring inputs (k0,k1) .. (k6,k7) of one stored word, as x's type, minus the
 // zero point.  The number q in the low bits of the constant's mantissa is 128 + q in bf16 (1024 + q in
-// f16) exactly, and so is the difference with 128 + z (1024 + z).
+// f16) exactly, and so is the difference with 128 + z (1024 + z).  The difference is one packed
+// multiply-add per pair (v * 1 - zero); the header's subtraction compiles to more.
 template <class T> struct W4Pairs;
 template <> struct W4Pairs<__nv_bfloat16> {
     static constexpr unsigned MAGIC = 0x43004300u;
-    static __device__ __forceinline__ unsigned sub(unsigned a, unsigned z)
+    static __device__ __forceinline__ unsigned add(unsigned a, unsigned z)
     {
-        __nv_bfloat162 r = __hsub2(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&z));
-        return *reinterpret_cast<unsigned *>(&r);
+        unsigned r;
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(0x3f803f80u), "r"(z));
+        return r;
     }
 };
 template <> struct W4Pairs<__half> {
     static constexpr unsigned MAGIC = 0x64006400u;
-    static __device__ __forceinline__ unsigned sub(unsigned a, unsigned z)
+    static __device__ __forceinline__ unsigned add(unsigned a, unsigned z)
     {
-        __half2 r = __hsub2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&z));
-        return *reinterpret_cast<unsigned *>(&r);
+        unsigned r;
+        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(0x3c003c00u), "r"(z));
+        return r;
     }
 };
+// minus the pair of the zero point z
 template <class T>
-__device__ __forceinline__ unsigned w4_zero_pair(int z) { return W4Pairs<T>::MAGIC | (unsigned)z | ((unsigned)z << 16); }
+__device__ __forceinline__ unsigned w4_zero_pair(int z) { return (W4Pairs<T>::MAGIC | 0x80008000u) | (unsigned)z | ((unsigned)z << 16); }
 template <class T>
 __device__ __forceinline__ void w4_unpack(unsigned word, unsigned zero_pair, unsigned (&p)[4])
 {
@@ -88,6 +92,6 @@ __device__ __forceinline__ void w4_unpack(unsigned word, unsigned zero_pair, uns
     for (int j = 0; j < 4; j++) {
         unsigned v;
         asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xea;" : "=r"(v) : "r"(word >> (4 * j)), "r"(W4Pairs<T>::MAGIC));   // (a & b) | c
-        p[j] = W4Pairs<T>::sub(v, zero_pair);
+        p[j] = W4Pairs<T>::add(v, zero_pair);
     }
 }
