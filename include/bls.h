@@ -421,7 +421,7 @@ bls_status_t bls_moe_combine_grad(const void *dout, int64_t ldd, const void *y, 
  *                      makes its whole group NaN.  Quotients are fp32.
  *   bls_w4_dequantize  the weights (q - z) * s in fp32, rounded once to dtype
  *   bls_w4_bytes       workspace of bls_w4_linear for these x, ldx and rows (256-byte aligned; 0 up to
- *                      32 rows, and when rows of x start at 16-byte boundaries)
+ *                      8 rows, and when rows of x start at 16-byte boundaries)
  *   bls_w4_linear      y[r][n] = act(bias[e][n] + sum over groups of s * sum of (q - z) * x[r][..]), e = the
  *                      matrix of row r: rows offsets[e] .. offsets[e + 1] - 1 (int32 [E + 1], as bls_moe_route
  *                      gives them; NULL with E = 1: all rows).  Rows from offsets[E] on are set to 0.

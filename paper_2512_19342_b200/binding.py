@@ -668,7 +668,7 @@ def bls_w4_linear(w4: W4, x: torch.Tensor, y: torch.Tensor, offsets: Optional[to
     py, ldy = _rows(y, "y", (rows, N), y.dtype)
     l = lib()
     ws, nbytes = None, 0
-    if rows > 32:                            # fewer rows never need a workspace
+    if rows > 8:                             # fewer rows never need a workspace
         size = C.c_size_t(0)
         _check(l.bls_w4_bytes(E, N, K, px, ldx, rows, C.byref(size)), "bls_w4_bytes")
         nbytes = size.value

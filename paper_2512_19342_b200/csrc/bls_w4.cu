@@ -396,7 +396,7 @@ bool w4_shape(int E, int N, int K, int group, W4Weights &w)
 }
 
 // Which kernel: by the rows that a matrix gets on average.
-bool many_rows(const W4Weights &w, int64_t rows) { return rows > 32ll * w.E; }
+bool many_rows(const W4Weights &w, int64_t rows) { return rows > 8ll * w.E; }
 
 template <class T, int GROUP>
 cudaError_t launch_rows_g(const W4Args &a, cudaStream_t s)

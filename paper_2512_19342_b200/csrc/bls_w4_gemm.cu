@@ -8,6 +8,9 @@
 // Weights are therefore never rounded, and a thread needs one scale per group, because its
 // accumulator lane is one output.
 //
+// With too few tiles for the SMs the CTAs of a cluster split K (SPLIT: one tile per cluster, the sums
+// meet through distributed shared memory in the order of the slices).
+//
 // Roles: warps 0-3 unpack, warps 4-11 scale and store, one thread of warp 12 loads (TMA for x, bulk
 // copies for the weight tile and its scales and zero points), one thread of warp 13 issues the
 // products.  Every wait is bounded by the clock: one that gives up latches BLS_ST_ETIMEOUT, all
@@ -87,9 +90,15 @@ __device__ __forceinline__ void gm_store(Y *at, long long ldy, int rows, const u
     }
 }
 
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 // grid: persistent, one CTA per SM at most; tiles are numbered over (matrix, row tile, output tile).
-template <class T, int GROUP, int HALVES>
-__global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ W4Args a)
+// SPLIT: one cluster of `slices` CTAs per tile, every CTA a slice of K.
+template <class T, int GROUP, int HALVES, bool SPLIT>
+__global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ W4Args a, int slices)
 {
     using Stage = GmStage<HALVES>;
     constexpr int STAGES = Stage::COUNT, GPT = W4_TILE / GROUP, ROWS = HALVES * GM_HALF;
@@ -103,7 +112,10 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                    d_full = a_empty + 8 * GM_SLOTS, d_empty = d_full + 16;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const W4Weights &w = a.w;
-    const int KT = w.KT;
+    // this CTA's first tile, the step to the next one, and its tiles of K
+    const int KT = w.KT, rank = SPLIT ? blockIdx.x % slices : 0, first_tile = SPLIT ? blockIdx.x / slices : blockIdx.x,
+              step = SPLIT ? gridDim.x / slices : gridDim.x, per = SPLIT ? (KT + slices - 1) / slices : KT,
+              k0 = SPLIT ? min(rank * per, KT) : 0, k1 = SPLIT ? min(k0 + per, KT) : KT;
 
     if (threadIdx.x == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
@@ -177,13 +189,13 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         if (warp == 12 && lane == 0) {
             unsigned s = 0, ph = 0, issued = 0;
             bool ok = true;
-            for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+            for (int i = first_tile; i < tiles && ok; i += step) {
                 const GmTile t = tile_of(i);
-                const uint8_t *q = w.q + ((size_t)t.e * w.NT + t.nt) * KT * W4_TILE_BYTES;
-                size_t g = (size_t)t.e * KT * GPT * w.NT * W4_TILE + t.nt * W4_TILE;
+                const uint8_t *q = w.q + (((size_t)t.e * w.NT + t.nt) * KT + k0) * W4_TILE_BYTES;
+                size_t g = ((size_t)t.e * KT + k0) * GPT * w.NT * W4_TILE + t.nt * W4_TILE;
                 const bool two = HALVES == 2 && t.rows > GM_HALF;
                 const unsigned bytes = W4_TILE_BYTES + (two ? 2 : 1) * GM_HALF_BYTES + GPT * W4_TILE * (w.zero ? 3 : 2);
-                for (int kt = 0; kt < KT; kt++) {
+                for (int kt = k0; kt < k1; kt++) {
                     ok = mb_wait(empty + 8 * s, ph ^ 1, a.status);
                     if (!ok) break;
                     const unsigned dst = smem + s * Stage::BYTES, side = smem + Stage::SCALE + s * Stage::SIDE, bar = full + 8 * s;
@@ -213,9 +225,9 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
             const bool leader = elect_one();
             unsigned s = 0, ph = 0, j = 0, jph = 0, used[2] = {0, 0}, b = 0;
             bool ok = true;
-            for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+            for (int i = first_tile; i < tiles && ok; i += step) {
                 const GmTile t = tile_of(i);
-                for (int kt = 0; kt < KT && ok; kt++) {
+                for (int kt = k0; kt < k1 && ok; kt++) {
                     ok = mb_wait(full + 8 * s, ph, a.status) && mb_wait(a_full + 8 * j, jph, a.status);
                     if (!ok) break;
                     const unsigned long long base = umma_desc(smem + s * Stage::BYTES);
@@ -260,8 +272,8 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         const unsigned swz = (unsigned)((r >> 1) & 3);
         unsigned s = 0, ph = 0, j = 0, jph = 0;
         bool ok = true;
-        for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-            for (int kt = 0; kt < KT; kt++) {
+        for (int i = first_tile; i < tiles && ok; i += step) {
+            for (int kt = k0; kt < k1; kt++) {
                 ok = mb_wait(full + 8 * s, ph, a.status);
                 if (!ok) break;
                 const unsigned src = smem + s * Stage::BYTES + Stage::W + r * 64;
@@ -311,14 +323,14 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         const unsigned lanes = (unsigned)(q4 * 32) << 16;
         unsigned s = 0, ph = 0, used[2] = {0, 0}, b = 0;
         bool ok = true;
-        for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+        for (int i = first_tile; i < tiles && ok; i += step) {
             const GmTile t = tile_of(i);
             unsigned long long tot[HALVES][2][16];                         // two rows each
             #pragma unroll
             for (int h = 0; h < HALVES; h++)
                 #pragma unroll
                 for (int c = 0; c < 32; c++) tot[h][c >> 4][c & 15] = 0ull;
-            for (int kt = 0; kt < KT && ok; kt++) {
+            for (int kt = k0; kt < k1 && ok; kt++) {
                 ok = mb_wait(full + 8 * s, ph, a.status);                  // the scales have arrived
                 if (!ok) break;
                 unsigned sc[GPT];
@@ -360,6 +372,14 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                 if (++s == STAGES) { s = 0; ph ^= 1; }
             }
             const int n = t.nt * W4_TILE + r;
+            if (SPLIT) {
+                // the slice's sums, [row][output], over the stages: every copy has arrived and every product has been read
+                #pragma unroll
+                for (int c = 0; c < 64; c++)
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(smem + ((part * 64 + c) * W4_TILE + r) * 4),
+                                 "r"((unsigned)(tot[0][c >> 5][c >> 1 & 15] >> (32 * (c & 1)))) : "memory");
+                continue;
+            }
             if (!ok || n >= w.N) continue;
             const float bias = a.bias ? a.bias[(size_t)t.e * w.N + n] : 0.f;
             #pragma unroll
@@ -374,6 +394,33 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                     else gm_store((__half *)a.y + at, a.ldy, t.rows - row, tot[h][p], bias, a.act);
                 }
         }
+        if (SPLIT) {
+            cluster_sync();
+            if (first_tile < tiles) {
+                // every CTA finishes 128 / slices outputs (slices is a power of two)
+                const GmTile t = tile_of(first_tile);
+                const int shift = 7 - (31 - __clz(slices));
+                for (int i = threadIdx.x - 128; i < t.rows << shift; i += 256) {
+                    const int row = i >> shift, o = (rank << shift) + (i & ((1 << shift) - 1)), n = t.nt * W4_TILE + o;
+                    if (n >= w.N) continue;
+                    const unsigned at = smem + (row * W4_TILE + o) * 4;
+                    float v = 0.f;
+                    for (int sl = 0; sl < slices; sl++) {
+                        float p;
+                        asm volatile("{\n\t.reg .u32 t;\n\tmapa.shared::cluster.u32 t, %1, %2;\n\tld.shared::cluster.f32 %0, [t];\n\t}" : "=f"(p) : "r"(at), "r"(sl) : "memory");
+                        v += p;
+                    }
+                    if (a.bias) v += a.bias[(size_t)t.e * w.N + n];
+                    w4_store(a.y, (size_t)(t.row0 + row) * a.ldy + n, a.y_dtype, w4_act(v, a.act));
+                }
+            }
+            cluster_sync();                                                // nobody reads this CTA's sums any more
+        }
+    }
+    if (SPLIT && (warp < 4 || warp >= 12)) {
+        __syncwarp();
+        cluster_sync();
+        cluster_sync();
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
@@ -409,25 +456,28 @@ int sm_count()
     return n > 0 ? n : 148;
 }
 
-template <class T, int GROUP, int HALVES>
-cudaError_t launch_tiles_h(const CUtensorMap &map, const W4Args &a, long long row_tiles, cudaStream_t s)
+template <class T, int GROUP, int HALVES, bool SPLIT>
+cudaError_t launch_tiles_h(const CUtensorMap &map, const W4Args &a, int grid, int slices, cudaStream_t s)
 {
     const size_t smem = 1024 + (size_t)GmStage<HALVES>::ALL;
-    cudaError_t e = cudaFuncSetAttribute(bls_w4_tiles_kernel<T, GROUP, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = cudaFuncSetAttribute(bls_w4_tiles_kernel<T, GROUP, HALVES, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    const int grid = (int)min(row_tiles * a.w.NT, (long long)sm_count());
-    return launch_serialised_smem(bls_w4_tiles_kernel<T, GROUP, HALVES>, dim3(grid), dim3(GM_THREADS), smem, s, map, a);
+    return launch_serialised_cluster(bls_w4_tiles_kernel<T, GROUP, HALVES, SPLIT>, dim3(grid), dim3(GM_THREADS), slices, smem, s, map, a, slices);
 }
 
 template <class T, int GROUP>
 cudaError_t launch_tiles_g(const CUtensorMap &map, const W4Args &a, cudaStream_t s)
 {
+    // upper bounds of the tiles: every matrix may end in a part of one
+    const long long ends = a.offsets ? min((long long)a.w.E, (long long)a.rows) : 0;
+    const long long small = ((a.rows + 127ll) / 128 + ends) * a.w.NT, big = ((a.rows + 255ll) / 256 + ends) * a.w.NT;
     // tiles of 256 rows unpack every weight for twice as many products; they are taken where enough of them remain
-    const long long big = (a.rows + 255) / 256;
-    const bool two = big * a.w.NT >= 2ll * sm_count();
-    // an upper bound of the row tiles: every matrix may end in a part of one
-    const long long per = two ? 256 : 128, row_tiles = (a.rows + per - 1) / per + (a.offsets ? min((long long)a.w.E, (long long)a.rows) : 0);
-    return two ? launch_tiles_h<T, GROUP, 2>(map, a, row_tiles, s) : launch_tiles_h<T, GROUP, 1>(map, a, row_tiles, s);
+    if ((a.rows + 255ll) / 256 * a.w.NT >= 2ll * sm_count())
+        return launch_tiles_h<T, GROUP, 2, false>(map, a, (int)min(big, (long long)sm_count()), 1, s);
+    int slices = 1;                                                // K is split while that leaves an SM for every slice of two tiles or more
+    while (slices < 8 && small * slices * 2 <= sm_count() && slices * 4 <= a.w.KT) slices *= 2;
+    if (slices > 1) return launch_tiles_h<T, GROUP, 1, true>(map, a, (int)small * slices, slices, s);
+    return launch_tiles_h<T, GROUP, 1, false>(map, a, (int)min(small, (long long)sm_count()), 1, s);
 }
 
 template <class T>
