@@ -1,6 +1,6 @@
 // The 4-bit product for many rows, on the tensor cores.
 //
-// A CTA computes 128 outputs x 128 or 256 rows: the weights are the M operand, unpacked by warps from
+// A CTA computes 128 outputs x 64, 128 or 256 rows: the weights are the M operand, unpacked by warps from
 // shared memory into tensor memory (integers q - z, exact in bf16 and f16), the rows of x are the
 // N operand in shared memory.  The accumulator of one group of inputs is complete after group / 16
 // instructions; it is then read back, scaled in fp32 and added to the running sums in registers,
@@ -21,17 +21,18 @@
 
 namespace {
 
-constexpr int GM_HALF = 128;                                  // rows of x per product instruction (its N)
 constexpr int GM_SLOTS = 4;                                   // tensor-memory slots of unpacked weights
-constexpr unsigned GM_HALF_BYTES = GM_HALF * W4_TILE * 2;     // one stage's x of 128 rows: two boxes of 64 inputs
 constexpr int GM_THREADS = 16 * 32;                           // warps 14 and 15 only fill the fourth warpgroup
-constexpr unsigned GM_TMEM_COLS = 512, GM_A_COL = 256;        // accumulators: columns 0..127 and 128..255; weights: 4 x 64 columns
+constexpr unsigned GM_TMEM_COLS = 512, GM_A_COL = 256;        // accumulators: columns 0..255; weights: 4 x 64 columns
 constexpr int GM_MAX_E = 1024;
 
-// A stage of 128 inputs: x, the weight tile, the scales and the zero points of its groups.
-template <int HALVES> struct GmStage {
-    static constexpr int COUNT = HALVES == 2 ? 3 : 5;         // what fits into 227 KB
-    static constexpr unsigned W = HALVES * GM_HALF_BYTES, BYTES = W + W4_TILE_BYTES;                        // x, weights
+// A tile has HALVES times COLS rows of x, COLS being the rows per product instruction (its N).  With one half of
+// 128 rows there are two accumulators, with one of 64 there are four: few rows make short products,
+// and more of them have to be under way.  A stage of 128 inputs: x, the weight tile, the scales and the zero points of its groups.
+template <int COLS, int HALVES> struct GmStage {
+    static constexpr int COUNT = HALVES == 2 ? 3 : COLS == 128 ? 5 : 8;                                     // what fits into 227 KB
+    static constexpr int BUFFERS = HALVES == 2 ? 2 : 256 / COLS;
+    static constexpr unsigned HALF = COLS * W4_TILE * 2, W = HALVES * HALF, BYTES = W + W4_TILE_BYTES;      // x (two boxes of 64 inputs), weights
     static constexpr unsigned SCALE = COUNT * BYTES, ZERO = 4 * W4_TILE * 2, SIDE = 4 * W4_TILE * 3;        // after all stages: scales, zero points
     static constexpr unsigned ALL = COUNT * (BYTES + SIDE);
 };
@@ -97,19 +98,20 @@ __device__ __forceinline__ void cluster_sync()
 
 // grid: persistent, one CTA per SM at most; tiles are numbered over (matrix, row tile, output tile).
 // SPLIT: one cluster of `slices` CTAs per tile, every CTA a slice of K.
-template <class T, int GROUP, int HALVES, bool SPLIT>
+template <class T, int GROUP, int COLS, int HALVES, bool SPLIT>
 __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ W4Args a, int slices)
 {
-    using Stage = GmStage<HALVES>;
-    constexpr int STAGES = Stage::COUNT, GPT = W4_TILE / GROUP, ROWS = HALVES * GM_HALF;
+    using Stage = GmStage<COLS, HALVES>;
+    constexpr int STAGES = Stage::COUNT, BUFS = Stage::BUFFERS, GPT = W4_TILE / GROUP, ROWS = HALVES * COLS, CHUNKS = COLS / 64;
+    constexpr unsigned HALF = Stage::HALF;
     extern __shared__ unsigned char gm_smem[];
-    __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * GM_SLOTS + 4];
+    __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * GM_SLOTS + 2 * BUFS];
     __shared__ unsigned tmem_slot;
     __shared__ int tile_end[GM_MAX_E];                            // row tiles of the matrices up to and including this one
     __shared__ int scan[16];
     const unsigned smem = (s_addr(gm_smem) + 1023u) & ~1023u;
     const unsigned full = s_addr(&bars[0]), empty = full + 8 * STAGES, a_full = empty + 8 * STAGES, a_empty = a_full + 8 * GM_SLOTS,
-                   d_full = a_empty + 8 * GM_SLOTS, d_empty = d_full + 16;
+                   d_full = a_empty + 8 * GM_SLOTS, d_empty = d_full + 8 * BUFS;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const W4Weights &w = a.w;
     // this CTA's first tile, the step to the next one, and its tiles of K
@@ -121,7 +123,7 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
         for (int s = 0; s < STAGES; s++) { mb_init(full + 8 * s, 1); mb_init(empty + 8 * s, 1 + 4 + 8); }
         for (int s = 0; s < GM_SLOTS; s++) { mb_init(a_full + 8 * s, 4); mb_init(a_empty + 8 * s, 1); }
-        for (int s = 0; s < 2; s++) { mb_init(d_full + 8 * s, 1); mb_init(d_empty + 8 * s, 8); }
+        for (int s = 0; s < BUFS; s++) { mb_init(d_full + 8 * s, 1); mb_init(d_empty + 8 * s, 8); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -193,8 +195,8 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                 const GmTile t = tile_of(i);
                 const uint8_t *q = w.q + (((size_t)t.e * w.NT + t.nt) * KT + k0) * W4_TILE_BYTES;
                 size_t g = ((size_t)t.e * KT + k0) * GPT * w.NT * W4_TILE + t.nt * W4_TILE;
-                const bool two = HALVES == 2 && t.rows > GM_HALF;
-                const unsigned bytes = W4_TILE_BYTES + (two ? 2 : 1) * GM_HALF_BYTES + GPT * W4_TILE * (w.zero ? 3 : 2);
+                const bool two = HALVES == 2 && t.rows > COLS;
+                const unsigned bytes = W4_TILE_BYTES + (two ? 2 : 1) * HALF + GPT * W4_TILE * (w.zero ? 3 : 2);
                 for (int kt = k0; kt < k1; kt++) {
                     ok = mb_wait(empty + 8 * s, ph ^ 1, a.status);
                     if (!ok) break;
@@ -203,10 +205,10 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                     bulk_load(dst + Stage::W, q, W4_TILE_BYTES, bar);
                     q += W4_TILE_BYTES;
                     tma_load_2d(dst, &map_x, bar, kt * W4_TILE, t.row0);
-                    tma_load_2d(dst + GM_HALF_BYTES / 2, &map_x, bar, kt * W4_TILE + 64, t.row0);
+                    tma_load_2d(dst + HALF / 2, &map_x, bar, kt * W4_TILE + 64, t.row0);
                     if (two) {
-                        tma_load_2d(dst + GM_HALF_BYTES, &map_x, bar, kt * W4_TILE, t.row0 + GM_HALF);
-                        tma_load_2d(dst + GM_HALF_BYTES + GM_HALF_BYTES / 2, &map_x, bar, kt * W4_TILE + 64, t.row0 + GM_HALF);
+                        tma_load_2d(dst + HALF, &map_x, bar, kt * W4_TILE, t.row0 + COLS);
+                        tma_load_2d(dst + HALF + HALF / 2, &map_x, bar, kt * W4_TILE + 64, t.row0 + COLS);
                     }
                     #pragma unroll
                     for (int gi = 0; gi < GPT; gi++) {
@@ -236,23 +238,23 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                     for (int gi = 0; gi < GPT; gi++) {
                         #pragma unroll
                         for (int h = 0; h < HALVES; h++) {
-                            const int rows = min(GM_HALF, t.rows - h * GM_HALF);
+                            const int rows = min(COLS, t.rows - h * COLS);
                             if (rows <= 0) continue;
                             if (HALVES == 2) b = h;
                             ok = ok && mb_wait(d_empty + 8 * b, (used[HALVES == 2 ? h : 0] & 1) ^ 1, a.status);
-                            if (HALVES == 2 || b == 1) used[HALVES == 2 ? h : 0]++;   // how often the buffer (HALVES == 1: both) has been filled
+                            if (HALVES == 2 || b == BUFS - 1) used[HALVES == 2 ? h : 0]++;    // how often the buffer (HALVES == 1: all) has been filled
                             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                             if (leader && ok) {
                                 const unsigned idesc = gm_idesc<T>((rows + 15) & ~15);
                                 #pragma unroll
                                 for (int k = 0; k < GROUP / 16; k++) {
                                     const int ks = gi * (GROUP / 16) + k;     // step of 16 inputs: box ks / 4, 32 bytes each
-                                    umma_f16_ta(tmem + b * 128, at + ks * 8,
-                                                base + (h * GM_HALF_BYTES + (ks >> 2) * (GM_HALF_BYTES / 2) + (ks & 3) * 32) / 16, idesc, k ? 1u : 0u);
+                                    umma_f16_ta(tmem + b * COLS, at + ks * 8,
+                                                base + (h * HALF + (ks >> 2) * (HALF / 2) + (ks & 3) * 32) / 16, idesc, k ? 1u : 0u);
                                 }
                                 umma_commit(d_full + 8 * b);
                             }
-                            if (HALVES == 1) b ^= 1;
+                            if (HALVES == 1) b = b == BUFS - 1 ? 0 : b + 1;
                         }
                     }
                     if (leader && ok) {
@@ -318,18 +320,18 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         }
     } else {
         regs_up<200>();
-        // scale and store: thread = output, 64 rows of x of every half
+        // scale and store: thread = output, half of the rows of x of every half of the tile
         const int q4 = warp & 3, part = (warp - 4) >> 2, r = q4 * 32 + lane;
         const unsigned lanes = (unsigned)(q4 * 32) << 16;
         unsigned s = 0, ph = 0, used[2] = {0, 0}, b = 0;
         bool ok = true;
         for (int i = first_tile; i < tiles && ok; i += step) {
             const GmTile t = tile_of(i);
-            unsigned long long tot[HALVES][2][16];                         // two rows each
+            unsigned long long tot[HALVES][CHUNKS][16];                         // two rows each
             #pragma unroll
             for (int h = 0; h < HALVES; h++)
                 #pragma unroll
-                for (int c = 0; c < 32; c++) tot[h][c >> 4][c & 15] = 0ull;
+                for (int c = 0; c < CHUNKS * 16; c++) tot[h][c >> 4][c & 15] = 0ull;
             for (int kt = k0; kt < k1 && ok; kt++) {
                 ok = mb_wait(full + 8 * s, ph, a.status);                  // the scales have arrived
                 if (!ok) break;
@@ -345,28 +347,30 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                     const unsigned long long s2 = (unsigned long long)sc[gi] << 32 | sc[gi];
                     #pragma unroll
                     for (int h = 0; h < HALVES; h++) {
-                        if (h * GM_HALF >= t.rows) continue;
+                        if (h * COLS >= t.rows) continue;
                         if (HALVES == 2) b = h;
                         ok = ok && mb_wait(d_full + 8 * b, used[HALVES == 2 ? h : 0] & 1, a.status);
-                        if (HALVES == 2 || b == 1) used[HALVES == 2 ? h : 0]++;
+                        if (HALVES == 2 || b == BUFS - 1) used[HALVES == 2 ? h : 0]++;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const bool busy = ok && h * GM_HALF + part * 64 < t.rows;          // the whole warp alike
-                        const unsigned src = tmem + lanes + b * 128 + part * 64;
+                        const bool busy = ok && h * COLS + part * (COLS / 2) < t.rows;     // the whole warp alike
+                        const unsigned src = tmem + lanes + b * COLS + part * (COLS / 2);
                         unsigned v[32];
                         if (busy) {
                             tmem_ld32(src, v);
-                            #pragma unroll
-                            for (int c = 0; c < 16; c++) tot[h][0][c] = fma2(s2, v[2 * c], v[2 * c + 1], tot[h][0][c]);
-                            tmem_ld32(src + 32, v);
+                            if (CHUNKS == 2) {
+                                #pragma unroll
+                                for (int c = 0; c < 16; c++) tot[h][0][c] = fma2(s2, v[2 * c], v[2 * c + 1], tot[h][0][c]);
+                                tmem_ld32(src + 32, v);
+                            }
                         }
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                         __syncwarp();
                         if (lane == 0) mb_arrive(d_empty + 8 * b);
                         if (busy) {
                             #pragma unroll
-                            for (int c = 0; c < 16; c++) tot[h][1][c] = fma2(s2, v[2 * c], v[2 * c + 1], tot[h][1][c]);
+                            for (int c = 0; c < 16; c++) tot[h][CHUNKS - 1][c] = fma2(s2, v[2 * c], v[2 * c + 1], tot[h][CHUNKS - 1][c]);
                         }
-                        if (HALVES == 1) b ^= 1;
+                        if (HALVES == 1) b = b == BUFS - 1 ? 0 : b + 1;
                     }
                 }
                 if (++s == STAGES) { s = 0; ph ^= 1; }
@@ -375,8 +379,8 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
             if (SPLIT) {
                 // the slice's sums, [row][output], over the stages: every copy has arrived and every product has been read
                 #pragma unroll
-                for (int c = 0; c < 64; c++)
-                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(smem + ((part * 64 + c) * W4_TILE + r) * 4),
+                for (int c = 0; c < COLS / 2; c++)
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(smem + ((part * (COLS / 2) + c) * W4_TILE + r) * 4),
                                  "r"((unsigned)(tot[0][c >> 5][c >> 1 & 15] >> (32 * (c & 1)))) : "memory");
                 continue;
             }
@@ -385,8 +389,8 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
             #pragma unroll
             for (int h = 0; h < HALVES; h++)
                 #pragma unroll
-                for (int p = 0; p < 2; p++) {
-                    const int row = h * GM_HALF + part * 64 + p * 32;
+                for (int p = 0; p < CHUNKS; p++) {
+                    const int row = h * COLS + part * (COLS / 2) + p * 32;
                     if (row >= t.rows) continue;
                     const size_t at = (size_t)(t.row0 + row) * a.ldy + n;
                     if (a.y_dtype == BLS_F32) gm_store((float *)a.y + at, a.ldy, t.rows - row, tot[h][p], bias, a.act);
@@ -399,19 +403,26 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
             if (first_tile < tiles) {
                 // every CTA finishes 128 / slices outputs (slices is a power of two)
                 const GmTile t = tile_of(first_tile);
-                const int shift = 7 - (31 - __clz(slices));
+                const int shift = 5 - (31 - __clz(slices));                // four outputs at a time
                 for (int i = threadIdx.x - 128; i < t.rows << shift; i += 256) {
-                    const int row = i >> shift, o = (rank << shift) + (i & ((1 << shift) - 1)), n = t.nt * W4_TILE + o;
-                    if (n >= w.N) continue;
+                    const int row = i >> shift, o = ((rank << shift) + (i & ((1 << shift) - 1))) * 4, n = t.nt * W4_TILE + o;
                     const unsigned at = smem + (row * W4_TILE + o) * 4;
-                    float v = 0.f;
-                    for (int sl = 0; sl < slices; sl++) {
-                        float p;
-                        asm volatile("{\n\t.reg .u32 t;\n\tmapa.shared::cluster.u32 t, %1, %2;\n\tld.shared::cluster.f32 %0, [t];\n\t}" : "=f"(p) : "r"(at), "r"(sl) : "memory");
-                        v += p;
-                    }
-                    if (a.bias) v += a.bias[(size_t)t.e * w.N + n];
-                    w4_store(a.y, (size_t)(t.row0 + row) * a.ldy + n, a.y_dtype, w4_act(v, a.act));
+                    float p[8][4], v[4] = {0.f, 0.f, 0.f, 0.f};
+                    #pragma unroll
+                    for (int sl = 0; sl < 8; sl++)
+                        if (sl < slices)
+                            asm volatile("{\n\t.reg .u32 t;\n\tmapa.shared::cluster.u32 t, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [t];\n\t}"
+                                         : "=f"(p[sl][0]), "=f"(p[sl][1]), "=f"(p[sl][2]), "=f"(p[sl][3]) : "r"(at), "r"(sl) : "memory");
+                    #pragma unroll
+                    for (int sl = 0; sl < 8; sl++)
+                        #pragma unroll
+                        for (int c = 0; c < 4; c++)
+                            if (sl < slices) v[c] += p[sl][c];
+                    #pragma unroll
+                    for (int c = 0; c < 4; c++)
+                        if (n + c < w.N)
+                            w4_store(a.y, (size_t)(t.row0 + row) * a.ldy + n + c, a.y_dtype,
+                                     w4_act(v[c] + (a.bias ? a.bias[(size_t)t.e * w.N + n + c] : 0.f), a.act));
                 }
             }
             cluster_sync();                                                // nobody reads this CTA's sums any more
@@ -456,34 +467,45 @@ int sm_count()
     return n > 0 ? n : 148;
 }
 
-template <class T, int GROUP, int HALVES, bool SPLIT>
-cudaError_t launch_tiles_h(const CUtensorMap &map, const W4Args &a, int grid, int slices, cudaStream_t s)
+template <class T, int GROUP, int COLS, int HALVES, bool SPLIT>
+cudaError_t launch_tiles_h(const W4Args &a, int grid, int slices, cudaStream_t s)
 {
-    const size_t smem = 1024 + (size_t)GmStage<HALVES>::ALL;
-    cudaError_t e = cudaFuncSetAttribute(bls_w4_tiles_kernel<T, GROUP, HALVES, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    CUtensorMap map;
+    if (!tc_make_map(&map, a.x, a.rows, a.w.K, a.ldx, COLS)) return cudaErrorInvalidValue;
+    const size_t smem = 1024 + (size_t)GmStage<COLS, HALVES>::ALL;
+    auto kernel = bls_w4_tiles_kernel<T, GROUP, COLS, HALVES, SPLIT>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    return launch_serialised_cluster(bls_w4_tiles_kernel<T, GROUP, HALVES, SPLIT>, dim3(grid), dim3(GM_THREADS), slices, smem, s, map, a, slices);
+    return launch_serialised_cluster(kernel, dim3(grid), dim3(GM_THREADS), slices, smem, s, map, a, slices);
+}
+
+// One half of COLS rows per tile; K is split while that leaves an SM for every slice of two tiles or more.
+template <class T, int GROUP, int COLS>
+cudaError_t launch_tiles_c(const W4Args &a, long long tiles, cudaStream_t s)
+{
+    int slices = 1;
+    while (slices < 8 && tiles * slices * 2 <= sm_count() && slices * 4 <= a.w.KT) slices *= 2;
+    if (slices > 1) return launch_tiles_h<T, GROUP, COLS, 1, true>(a, (int)tiles * slices, slices, s);
+    return launch_tiles_h<T, GROUP, COLS, 1, false>(a, (int)min(tiles, (long long)sm_count()), 1, s);
 }
 
 template <class T, int GROUP>
-cudaError_t launch_tiles_g(const CUtensorMap &map, const W4Args &a, cudaStream_t s)
+cudaError_t launch_tiles_g(const W4Args &a, cudaStream_t s)
 {
     // upper bounds of the tiles: every matrix may end in a part of one
-    const long long ends = a.offsets ? min((long long)a.w.E, (long long)a.rows) : 0;
-    const long long small = ((a.rows + 127ll) / 128 + ends) * a.w.NT, big = ((a.rows + 255ll) / 256 + ends) * a.w.NT;
+    const long long layers = min((long long)a.w.E, (long long)a.rows), ends = a.offsets ? layers : 0;
+    const auto tiles = [&](int rows) { return ((a.rows + rows - 1ll) / rows + ends) * a.w.NT; };
     // tiles of 256 rows unpack every weight for twice as many products; they are taken where enough of them remain
     if ((a.rows + 255ll) / 256 * a.w.NT >= 2ll * sm_count())
-        return launch_tiles_h<T, GROUP, 2, false>(map, a, (int)min(big, (long long)sm_count()), 1, s);
-    int slices = 1;                                                // K is split while that leaves an SM for every slice of two tiles or more
-    while (slices < 8 && small * slices * 2 <= sm_count() && slices * 4 <= a.w.KT) slices *= 2;
-    if (slices > 1) return launch_tiles_h<T, GROUP, 1, true>(map, a, (int)small * slices, slices, s);
-    return launch_tiles_h<T, GROUP, 1, false>(map, a, (int)min(small, (long long)sm_count()), 1, s);
+        return launch_tiles_h<T, GROUP, 128, 2, false>(a, (int)min(tiles(256), (long long)sm_count()), 1, s);
+    if (a.rows <= 64 * layers) return launch_tiles_c<T, GROUP, 64>(a, tiles(64), s);
+    return launch_tiles_c<T, GROUP, 128>(a, tiles(128), s);
 }
 
 template <class T>
-cudaError_t launch_tiles(const CUtensorMap &map, const W4Args &a, cudaStream_t s)
+cudaError_t launch_tiles(const W4Args &a, cudaStream_t s)
 {
-    return a.w.group == 32 ? launch_tiles_g<T, 32>(map, a, s) : a.w.group == 64 ? launch_tiles_g<T, 64>(map, a, s) : launch_tiles_g<T, 128>(map, a, s);
+    return a.w.group == 32 ? launch_tiles_g<T, 32>(a, s) : a.w.group == 64 ? launch_tiles_g<T, 64>(a, s) : launch_tiles_g<T, 128>(a, s);
 }
 
 }  // namespace
@@ -504,7 +526,5 @@ cudaError_t w4_tiles(W4Args a, int x_dtype, void *workspace, cudaStream_t s)
         if (e != cudaSuccess) return e;
         a.x = workspace; a.ldx = ldo; a.x_pieces = 1;
     }
-    CUtensorMap map;
-    if (!tc_make_map(&map, a.x, a.rows, a.w.K, a.ldx, GM_HALF)) return cudaErrorInvalidValue;
-    return x_dtype == BLS_BF16 ? launch_tiles<__nv_bfloat16>(map, a, s) : launch_tiles<__half>(map, a, s);
+    return x_dtype == BLS_BF16 ? launch_tiles<__nv_bfloat16>(a, s) : launch_tiles<__half>(a, s);
 }
