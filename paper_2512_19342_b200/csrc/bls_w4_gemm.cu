@@ -78,15 +78,13 @@ template <class T> __device__ __forceinline__ unsigned gm_idesc(int n)
     return (1u << 4) | (f << 7) | (f << 10) | ((unsigned)(n >> 3) << 17) | ((unsigned)(128 >> 4) << 24);
 }
 
-// 32 results of one output, one per row of x, from `at` on.
+// 32 results of one output, one per row of x, from `at` on; results below `least` become it (ReLU: 0, else minus infinity).
 template <class Y>
-__device__ __forceinline__ void gm_store(Y *at, long long ldy, int rows, const unsigned long long (&tot)[16], float bias, int act)
+__device__ __forceinline__ void gm_store(Y *at, long long ldy, int rows, const float (&v)[32], float least)
 {
     #pragma unroll
     for (int c = 0; c < 32; c++) {
-        float v = __uint_as_float((unsigned)(tot[c >> 1] >> (32 * (c & 1)))) + bias;
-        if (act) v = w4_act(v, act);
-        if (c < rows) *at = from_float<Y>(v);
+        if (c < rows) *at = from_float<Y>(v[c] < least ? least : v[c]);
         at += ldy;
     }
 }
@@ -393,9 +391,17 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                     const int row = h * COLS + part * (COLS / 2) + p * 32;
                     if (row >= t.rows) continue;
                     const size_t at = (size_t)(t.row0 + row) * a.ldy + n;
-                    if (a.y_dtype == BLS_F32) gm_store((float *)a.y + at, a.ldy, t.rows - row, tot[h][p], bias, a.act);
-                    else if (a.y_dtype == BLS_BF16) gm_store((__nv_bfloat16 *)a.y + at, a.ldy, t.rows - row, tot[h][p], bias, a.act);
-                    else gm_store((__half *)a.y + at, a.ldy, t.rows - row, tot[h][p], bias, a.act);
+                    float v[32];
+                    #pragma unroll
+                    for (int c = 0; c < 32; c++) v[c] = __uint_as_float((unsigned)(tot[h][p][c >> 1] >> (32 * (c & 1)))) + bias;
+                    if (a.act == 2) {
+                        #pragma unroll
+                        for (int c = 0; c < 32; c++) v[c] = w4_act(v[c], 2);
+                    }
+                    const float least = a.act == 1 ? 0.f : __int_as_float(0xff800000);
+                    if (a.y_dtype == BLS_F32) gm_store((float *)a.y + at, a.ldy, t.rows - row, v, least);
+                    else if (a.y_dtype == BLS_BF16) gm_store((__nv_bfloat16 *)a.y + at, a.ldy, t.rows - row, v, least);
+                    else gm_store((__half *)a.y + at, a.ldy, t.rows - row, v, least);
                 }
         }
         if (SPLIT) {
