@@ -162,8 +162,59 @@ template <> __device__ __forceinline__ float from_f<float>(float v) { return v; 
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
 
-// V elements of T that move as one piece (16 bytes, or one element where rows do not allow it).
-template <class T, int V> struct alignas(sizeof(T) * V) Piece { T v[V]; };
+// V elements of T that move as one piece: 16 bytes, or one element where rows do not allow it.  Pieces are kept as
+// they were loaded and taken apart as fp32 only where they are summed.
+template <class T, int V> struct Piece {
+    using Raw = T;
+    static __device__ __forceinline__ void floats(const Raw &r, float (&f)[V]) { f[0] = to_f(r); }
+    static __device__ __forceinline__ Raw from(const float (&f)[V]) { return from_f<T>(f[0]); }
+};
+template <> struct Piece<float, 4> {
+    using Raw = float4;
+    static __device__ __forceinline__ void floats(const Raw &r, float (&f)[4]) { f[0] = r.x; f[1] = r.y; f[2] = r.z; f[3] = r.w; }
+    static __device__ __forceinline__ Raw from(const float (&f)[4]) { return make_float4(f[0], f[1], f[2], f[3]); }
+};
+template <> struct Piece<__nv_bfloat16, 8> {
+    using Raw = uint4;
+    static __device__ __forceinline__ void floats(const Raw &r, float (&f)[8])
+    {
+        const unsigned u[4] = {r.x, r.y, r.z, r.w};
+        #pragma unroll
+        for (int i = 0; i < 4; i++) { f[2 * i] = __uint_as_float(u[i] << 16); f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+    }
+    static __device__ __forceinline__ Raw from(const float (&f)[8])
+    {
+        unsigned u[4];
+        #pragma unroll
+        for (int i = 0; i < 4; i++) {
+            __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+            u[i] = *reinterpret_cast<unsigned *>(&h);
+        }
+        return make_uint4(u[0], u[1], u[2], u[3]);
+    }
+};
+template <> struct Piece<__half, 8> {
+    using Raw = uint4;
+    static __device__ __forceinline__ void floats(const Raw &r, float (&f)[8])
+    {
+        const unsigned u[4] = {r.x, r.y, r.z, r.w};
+        #pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float2 g = __half22float2(*reinterpret_cast<const __half2 *>(&u[i]));
+            f[2 * i] = g.x; f[2 * i + 1] = g.y;
+        }
+    }
+    static __device__ __forceinline__ Raw from(const float (&f)[8])
+    {
+        unsigned u[4];
+        #pragma unroll
+        for (int i = 0; i < 4; i++) {
+            __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+            u[i] = *reinterpret_cast<unsigned *>(&h);
+        }
+        return make_uint4(u[0], u[1], u[2], u[3]);
+    }
+};
 
 struct MoveArgs {
     const void *a;              // dispatch: x; combine: y; gradient: dout
@@ -173,99 +224,173 @@ struct MoveArgs {
     const int *place, *total;   // total: number of sorted rows (device)
     const float *w;
     float *dw;
-    long long tokens, rows;
-    int k, pieces;              // pieces of a row
+    int tokens, rows, k;
+    int pieces;                 // pieces of a row
+    int lanes_log;              // threads of a token (of a slot)
 };
+
+// Who does what: 1 << lanes_log neighbouring threads take a token, its pieces `lane`, `lane` + lanes, .. .  Blocks
+// share the tokens and, along the other axis, the turns of a long row (the gradient: the slots), so that no
+// index is divided.
+struct MoveLane {
+    int token, step, lane, lanes;
+    __device__ __forceinline__ MoveLane(const MoveArgs &m, int block, int blocks)
+    {
+        lanes = 1 << m.lanes_log;
+        lane = threadIdx.x & (lanes - 1);
+        const int per = MOVE_THREADS >> m.lanes_log;                          // tokens of a block
+        token = block * per + (threadIdx.x >> m.lanes_log);
+        step = blocks * per;
+    }
+};
+
+template <class T, int V> using MP = typename Piece<T, V>::Raw;
 
 // Sets the rows of o from *total on to zero; the blocks of the grid share them.
 template <class T, int V>
-__device__ __forceinline__ void zero_tail(const MoveArgs &m)
+__device__ __forceinline__ void zero_tail(const MoveArgs &m, const MoveLane &l, int part, int parts)
 {
+    const float none[V] = {};
+    const MP<T, V> z = Piece<T, V>::from(none);
     const long long first = max(0, *m.total);
-    for (long long i = first * m.pieces + (long long)blockIdx.x * blockDim.x + threadIdx.x; i < m.rows * m.pieces; i += (long long)gridDim.x * blockDim.x) {
-        Piece<T, V> z;
-        #pragma unroll
-        for (int c = 0; c < V; c++) z.v[c] = from_f<T>(0.f);
-        *(Piece<T, V> *)((T *)m.o + i / m.pieces * m.ldo + i % m.pieces * V) = z;
-    }
+    for (long long r = first + l.token; r < m.rows; r += l.step)
+        for (int p = part * l.lanes + l.lane; p < m.pieces; p += parts * l.lanes)
+            *(MP<T, V> *)((T *)m.o + r * m.ldo + (long long)p * V) = z;
 }
 
-// One thread per piece of a token: read once, written to the token's k places.
+// A thread reads U pieces of a token and writes them to the token's k places: x is read once.
 template <class T, int V>
-__global__ void __launch_bounds__(MOVE_THREADS) bls_moe_dispatch_kernel(MoveArgs m)
+__global__ void __launch_bounds__(MOVE_THREADS) bls_moe_dispatch_kernel(const __grid_constant__ MoveArgs m)
 {
     stream_order_enter();
-    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < m.tokens * m.pieces; i += (long long)gridDim.x * blockDim.x) {
-        const long long t = i / m.pieces;
-        const long long c = i % m.pieces * V;
-        const Piece<T, V> p = *(const Piece<T, V> *)((const T *)m.a + t * m.lda + c);
-        for (int j = 0; j < m.k; j++) {
-            const int at = m.place[t * m.k + j];
-            if (at >= 0 && at < m.rows) *(Piece<T, V> *)((T *)m.o + at * m.ldo + c) = p;
-        }
-    }
-    zero_tail<T, V>(m);
-}
-
-template <class T, int V>
-__global__ void __launch_bounds__(MOVE_THREADS) bls_moe_combine_kernel(MoveArgs m)
-{
-    stream_order_enter();
-    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < m.tokens * m.pieces; i += (long long)gridDim.x * blockDim.x) {
-        const long long t = i / m.pieces;
-        const long long c = i % m.pieces * V;
-        float acc[V];
-        #pragma unroll
-        for (int e = 0; e < V; e++) acc[e] = 0.f;
-        for (int j = 0; j < m.k; j++) {
-            const int at = m.place[t * m.k + j];
-            if (at < 0 || at >= m.rows) continue;
-            const float w = m.w ? m.w[t * m.k + j] : 1.f;
-            const Piece<T, V> p = *(const Piece<T, V> *)((const T *)m.a + at * m.lda + c);
+    constexpr int U = V == 1 ? 4 : 1;
+    const MoveLane l(m, blockIdx.y, gridDim.y);
+    for (long long t = l.token; t < m.tokens; t += l.step) {
+        const int *place = m.place + t * m.k;
+        for (int p0 = blockIdx.x * l.lanes * U + l.lane; p0 < m.pieces; p0 += gridDim.x * l.lanes * U) {
+            MP<T, V> v[U];
             #pragma unroll
-            for (int e = 0; e < V; e++) acc[e] = fmaf(w, to_f(p.v[e]), acc[e]);
-        }
-        Piece<T, V> r;
-        #pragma unroll
-        for (int e = 0; e < V; e++) r.v[e] = from_f<T>(acc[e]);
-        *(Piece<T, V> *)((T *)m.o + t * m.ldo + c) = r;
-    }
-}
-
-// One warp per slot: dy = w * dout and dw = <dout, y> in one pass over the row.
-template <class T, int V>
-__global__ void __launch_bounds__(MOVE_THREADS) bls_moe_combine_grad_kernel(MoveArgs m)
-{
-    stream_order_enter();
-    const int lane = threadIdx.x & 31;
-    const long long warps = (long long)gridDim.x * (blockDim.x >> 5);
-    for (long long s = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5); s < m.tokens * m.k; s += warps) {
-        const int at = m.place[s];
-        const bool kept = at >= 0 && at < m.rows;
-        float dot = 0.f;
-        if (kept) {
-            const float w = m.w ? m.w[s] : 1.f;
-            const T *d = (const T *)m.a + s / m.k * m.lda;
-            for (int i = lane; i < m.pieces; i += 32) {
-                const Piece<T, V> g = *(const Piece<T, V> *)(d + i * V);
-                if (m.dw) {
-                    const Piece<T, V> y = *(const Piece<T, V> *)((const T *)m.b + at * m.ldb + i * V);
-                    #pragma unroll
-                    for (int e = 0; e < V; e++) dot = fmaf(to_f(g.v[e]), to_f(y.v[e]), dot);
-                }
-                Piece<T, V> r;
+            for (int u = 0; u < U; u++)
+                if (p0 + u * l.lanes < m.pieces) v[u] = *(const MP<T, V> *)((const T *)m.a + t * m.lda + (long long)(p0 + u * l.lanes) * V);
+            for (int j = 0; j < m.k; j++) {
+                const int at = __ldg(place + j);
+                if ((unsigned)at >= (unsigned)m.rows) continue;
+                T *o = (T *)m.o + at * m.ldo + (long long)p0 * V;
                 #pragma unroll
-                for (int e = 0; e < V; e++) r.v[e] = from_f<T>(w * to_f(g.v[e]));
-                *(Piece<T, V> *)((T *)m.o + at * m.ldo + i * V) = r;
+                for (int u = 0; u < U; u++)
+                    if (p0 + u * l.lanes < m.pieces) *(MP<T, V> *)(o + (long long)u * l.lanes * V) = v[u];
             }
         }
-        if (m.dw) {
+    }
+    zero_tail<T, V>(m, l, blockIdx.x, gridDim.x);
+}
+
+// A thread sums U pieces of a token over its k rows, several rows' pieces on their way at a time, in the order of the slots.
+template <class T, int V>
+__global__ void __launch_bounds__(MOVE_THREADS) bls_moe_combine_kernel(const __grid_constant__ MoveArgs m)
+{
+    stream_order_enter();
+    constexpr int U = V == 1 ? 4 : 1, J = 4;
+    const MoveLane l(m, blockIdx.y, gridDim.y);
+    for (long long t = l.token; t < m.tokens; t += l.step) {
+        const int *place = m.place + t * m.k;
+        const float *weight = m.w + t * m.k;
+        for (int p0 = blockIdx.x * l.lanes * U + l.lane; p0 < m.pieces; p0 += gridDim.x * l.lanes * U) {
+            float acc[U][V];
             #pragma unroll
-            for (int o = 16; o; o >>= 1) dot += __shfl_xor_sync(~0u, dot, o);
-            if (lane == 0) m.dw[s] = kept ? dot : 0.f;
+            for (int u = 0; u < U; u++)
+                #pragma unroll
+                for (int e = 0; e < V; e++) acc[u][e] = 0.f;
+            for (int j0 = 0; j0 < m.k; j0 += J) {
+                MP<T, V> v[J][U];
+                int at[J];
+                float w[J];
+                #pragma unroll
+                for (int j = 0; j < J; j++) {
+                    at[j] = j0 + j < m.k ? __ldg(place + j0 + j) : -1;
+                    w[j] = m.w && j0 + j < m.k ? __ldg(weight + j0 + j) : 1.f;
+                }
+                #pragma unroll
+                for (int j = 0; j < J; j++)
+                    if ((unsigned)at[j] < (unsigned)m.rows)
+                        #pragma unroll
+                        for (int u = 0; u < U; u++)
+                            if (p0 + u * l.lanes < m.pieces)
+                                v[j][u] = *(const MP<T, V> *)((const T *)m.a + at[j] * m.lda + (long long)(p0 + u * l.lanes) * V);
+                #pragma unroll
+                for (int j = 0; j < J; j++)
+                    if ((unsigned)at[j] < (unsigned)m.rows)
+                        #pragma unroll
+                        for (int u = 0; u < U; u++) {
+                            float f[V];
+                            Piece<T, V>::floats(v[j][u], f);
+                            #pragma unroll
+                            for (int e = 0; e < V; e++) acc[u][e] = fmaf(w[j], f[e], acc[u][e]);
+                        }
+            }
+            #pragma unroll
+            for (int u = 0; u < U; u++) {
+                if (p0 + u * l.lanes >= m.pieces) break;
+                *(MP<T, V> *)((T *)m.o + t * m.ldo + (long long)(p0 + u * l.lanes) * V) = Piece<T, V>::from(acc[u]);
+            }
         }
     }
-    zero_tail<T, V>(m);
+}
+
+// The lanes of a token take its slots (blockIdx.y: which of them): dy = w * dout and dw = <dout, y> in one pass over the
+// row, U pieces at a time.  Blocks of the same slot number run together: their rows lie close to
+// one another in y and dy when neighbouring tokens go to the same expert.
+template <class T, int V>
+__global__ void __launch_bounds__(MOVE_THREADS) bls_moe_combine_grad_kernel(const __grid_constant__ MoveArgs m)
+{
+    stream_order_enter();
+    constexpr int U = V == 1 ? 8 : 4;
+    const MoveLane l(m, blockIdx.x, gridDim.x);
+    // all lanes of a warp take the same number of turns (the sums below are shuffled over the warp)
+    const int sub = threadIdx.x % 32 >> m.lanes_log;
+    for (long long t0 = l.token - sub; t0 < m.tokens; t0 += l.step) {
+        const long long t = t0 + sub;
+        const T *d = (const T *)m.a + t * m.lda;
+        for (int j = blockIdx.y; j < m.k; j += gridDim.y) {
+            const long long s = t * m.k + j;
+            const int at = t < m.tokens ? __ldg(m.place + s) : -1;
+            const bool kept = (unsigned)at < (unsigned)m.rows;
+            float dot = 0.f;
+            if (kept) {
+                const float w = m.w ? __ldg(m.w + s) : 1.f;
+                const T *y = (const T *)m.b + at * m.ldb;
+                T *o = (T *)m.o + at * m.ldo;
+                for (int p0 = l.lane; p0 < m.pieces; p0 += l.lanes * U) {
+                    MP<T, V> g[U], v[U];
+                    #pragma unroll
+                    for (int u = 0; u < U; u++)
+                        if (p0 + u * l.lanes < m.pieces) {
+                            g[u] = *(const MP<T, V> *)(d + (long long)(p0 + u * l.lanes) * V);
+                            if (m.dw) v[u] = *(const MP<T, V> *)(y + (long long)(p0 + u * l.lanes) * V);
+                        }
+                    #pragma unroll
+                    for (int u = 0; u < U; u++)
+                        if (p0 + u * l.lanes < m.pieces) {
+                            float f[V], h[V];
+                            Piece<T, V>::floats(g[u], f);
+                            if (m.dw) {
+                                Piece<T, V>::floats(v[u], h);
+                                #pragma unroll
+                                for (int e = 0; e < V; e++) dot = fmaf(f[e], h[e], dot);
+                            }
+                            #pragma unroll
+                            for (int e = 0; e < V; e++) f[e] *= w;
+                            *(MP<T, V> *)(o + (long long)(p0 + u * l.lanes) * V) = Piece<T, V>::from(f);
+                        }
+                }
+            }
+            if (m.dw) {
+                for (int x = l.lanes >> 1; x; x >>= 1) dot += __shfl_xor_sync(~0u, dot, x);
+                if (l.lane == 0 && t < m.tokens) m.dw[s] = kept ? dot : 0.f;
+            }
+        }
+    }
+    zero_tail<T, V>(m, l, blockIdx.y, gridDim.y);
 }
 
 bool whole_pieces(const void *p, long long ld, int dim, int elem)
@@ -279,11 +404,18 @@ template <class T, int V>
 cudaError_t launch_move_v(int what, MoveArgs m, int dim, cudaStream_t s)
 {
     m.pieces = dim / V;
-    const long long items = what == MOVE_GRAD ? m.tokens * m.k * 32 : m.tokens * m.pieces;
-    const unsigned blocks = (unsigned)max(1ll, min((items + MOVE_THREADS - 1) / MOVE_THREADS, 148ll * 32));
+    // no more threads than a row has pieces; a slot's gradient is summed inside a warp, and single elements are
+    // taken by warps with more of them each
+    m.lanes_log = what == MOVE_GRAD || V == 1 ? 5 : 8;
+    while (m.lanes_log > 2 && 1 << (m.lanes_log - 1) >= m.pieces) m.lanes_log--;
+    const long long per = MOVE_THREADS >> m.lanes_log, most = 148 * 32;
+    const unsigned blocks = (unsigned)max(1ll, min((m.tokens + per - 1) / per, most));
+    const int turn = (V == 1 ? 4 : 1) << m.lanes_log;
+    const dim3 grid = what == MOVE_GRAD ? dim3(blocks, (unsigned)max(1ll, min((long long)m.k, most / blocks))) :
+                                         dim3((unsigned)min((m.pieces + turn - 1) / turn, 1024), blocks);
     void (*kernel)(MoveArgs) = what == MOVE_DISPATCH ? bls_moe_dispatch_kernel<T, V> :
                                what == MOVE_COMBINE ? bls_moe_combine_kernel<T, V> : bls_moe_combine_grad_kernel<T, V>;
-    return launch_serialised(kernel, dim3(blocks), dim3(MOVE_THREADS), s, m);
+    return launch_serialised(kernel, grid, dim3(MOVE_THREADS), s, m);
 }
 
 bls_status_t launch_move(int what, const MoveArgs &m, int dtype, int dim, bool whole, cudaStream_t s)
@@ -352,7 +484,7 @@ bls_status_t bls_moe_dispatch(const void *x, int64_t ldx, int dtype, const int32
     if (rows == 0) return BLS_OK;
     MoveArgs m = {};
     m.a = x; m.lda = ldx; m.o = y; m.ldo = ldy; m.place = place; m.total = offsets + n_experts;
-    m.tokens = tokens; m.rows = rows; m.k = k;
+    m.tokens = (int)tokens; m.rows = (int)rows; m.k = k;
     const int eb = elem_bytes(dtype);
     return launch_move(MOVE_DISPATCH, m, dtype, dim, whole_pieces(x, ldx, dim, eb) && whole_pieces(y, ldy, dim, eb), (cudaStream_t)cuda_stream);
 }
@@ -364,7 +496,7 @@ bls_status_t bls_moe_combine(const void *y, int64_t ldy, int64_t rows, int dtype
     if (tokens == 0) return BLS_OK;
     MoveArgs m = {};
     m.a = y; m.lda = ldy; m.o = out; m.ldo = ldo; m.place = place; m.w = w;
-    m.tokens = tokens; m.rows = rows; m.k = k;
+    m.tokens = (int)tokens; m.rows = (int)rows; m.k = k;
     const int eb = elem_bytes(dtype);
     return launch_move(MOVE_COMBINE, m, dtype, dim, whole_pieces(y, ldy, dim, eb) && whole_pieces(out, ldo, dim, eb), (cudaStream_t)cuda_stream);
 }
@@ -379,7 +511,7 @@ bls_status_t bls_moe_combine_grad(const void *dout, int64_t ldd, const void *y, 
     if (rows == 0 && !(dw && tokens)) return BLS_OK;
     MoveArgs m = {};
     m.a = dout; m.lda = ldd; m.b = y; m.ldb = ldy; m.o = dy; m.ldo = lddy; m.place = place; m.total = offsets + n_experts;
-    m.w = w; m.dw = dw; m.tokens = tokens; m.rows = rows; m.k = k;
+    m.w = w; m.dw = dw; m.tokens = (int)tokens; m.rows = (int)rows; m.k = k;
     const int eb = elem_bytes(dtype);
     const bool whole = whole_pieces(dout, ldd, dim, eb) && whole_pieces(dy, lddy, dim, eb) && (!dw || whole_pieces(y, ldy, dim, eb));
     return launch_move(MOVE_GRAD, m, dtype, dim, whole, (cudaStream_t)cuda_stream);

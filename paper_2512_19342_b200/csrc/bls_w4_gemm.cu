@@ -61,7 +61,7 @@ __device__ __forceinline__ bool elect_one()
     return p != 0;
 }
 // Registers move to the warps that hold the running sums: 512 threads start with 128 each (512 per four
-// threads, one of each warpgroup); 80 + 2 x 200 + 32 = 512.
+// threads, one of each warpgroup); 64 + 2 x 208 + 32 = 512.
 template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
             }
         }
     } else if (warp < 4) {
-        regs_down<80>();
+        regs_down<64>();
         // unpack: thread = output row of the weight tile = lane of tensor memory
         const int r = warp * 32 + lane;
         const unsigned swz = (unsigned)((r >> 1) & 3);
@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
             }
         }
     } else {
-        regs_up<200>();
+        regs_up<208>();
         // scale and store: thread = output, half of the rows of x of every half of the tile
         const int q4 = warp & 3, part = (warp - 4) >> 2, r = q4 * 32 + lane;
         const unsigned lanes = (unsigned)(q4 * 32) << 16;
