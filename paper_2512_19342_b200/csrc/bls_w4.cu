@@ -479,6 +479,7 @@ bls_status_t bls_w4_linear(const uint8_t *q, const void *scale, const uint8_t *z
     a.w.q = q; a.w.scale = (const __nv_bfloat16 *)scale; a.w.zero = zero;
     a.x = x; a.ldx = ldx; a.rows = (int)rows; a.x_pieces = ((uintptr_t)x & 15) == 0 && ldx % 8 == 0;
     a.offsets = offsets; a.bias = bias; a.act = act; a.y = y; a.y_dtype = y_dtype; a.ldy = ldy; a.status = status;
+    a.y_pieces = y_dtype != BLS_F32 && ((uintptr_t)y & 15) == 0 && ldy % 8 == 0 && N % 8 == 0;
     cudaError_t r = many_rows(a.w, rows) ? w4_tiles(a, x_dtype, workspace, (cudaStream_t)cuda_stream) :
                     x_dtype == BLS_BF16 ? launch_rows<__nv_bfloat16>(a, (cudaStream_t)cuda_stream) : launch_rows<__half>(a, (cudaStream_t)cuda_stream);
     return r == cudaSuccess ? BLS_OK : BLS_ECUDA;

@@ -26,6 +26,7 @@ struct W4Args {
     int act;
     void *y;
     int y_dtype;
+    int y_pieces;                            // 16-bit rows of y (and N) are whole 16-byte pieces
     long long ldy;
     int *status;
 };

@@ -26,15 +26,25 @@ constexpr int GM_THREADS = 16 * 32;                           // warps 14 and 15
 constexpr unsigned GM_TMEM_COLS = 512, GM_A_COL = 256;        // accumulators: columns 0..255; weights: 4 x 64 columns
 constexpr int GM_MAX_E = 1024;
 
+struct GmRest {
+    unsigned long long bars[2 * 8 + 2 * GM_SLOTS + 2 * 4];        // at most 8 stages and 4 accumulators
+    int tile_end[GM_MAX_E];                                       // row tiles of the matrices up to and including this one
+    int scan[16];
+    unsigned tmem_slot;
+};
+
 // A tile has HALVES times COLS rows of x, COLS being the rows per product instruction (its N).  With one half of
 // 128 rows there are two accumulators, with one of 64 there are four: few rows make short products,
 // and more of them have to be under way.  A stage of 128 inputs: x, the weight tile, the scales and the zero points of its groups.
-template <int COLS, int HALVES> struct GmStage {
+template <int GROUP, int COLS, int HALVES> struct GmStage {
     static constexpr int COUNT = HALVES == 2 ? 3 : COLS == 128 ? 5 : 8;                                     // what fits into 227 KB
     static constexpr int BUFFERS = HALVES == 2 ? 2 : 256 / COLS;
     static constexpr unsigned HALF = COLS * W4_TILE * 2, W = HALVES * HALF, BYTES = W + W4_TILE_BYTES;      // x (two boxes of 64 inputs), weights
-    static constexpr unsigned SCALE = COUNT * BYTES, ZERO = 4 * W4_TILE * 2, SIDE = 4 * W4_TILE * 3;        // after all stages: scales, zero points
-    static constexpr unsigned ALL = COUNT * (BYTES + SIDE);
+    // after all stages: scales and zero points, 64-byte rows of results for each of the eight storing warps, and the rest
+    static constexpr int GPT = W4_TILE / GROUP, STORE_ROWS = HALVES == 2 && GROUP == 32 ? 4 : 8;
+    static constexpr unsigned SCALE = COUNT * BYTES, ZERO = GPT * W4_TILE * 2, SIDE = GPT * W4_TILE * 3,
+                              STORE = SCALE + COUNT * SIDE, REST = STORE + 8 * STORE_ROWS * 64, ALL = REST + sizeof(GmRest);
+    static_assert(ALL <= 232448, "shared memory of a CTA");
 };
 
 struct GmTile { int e, row0, rows, nt; };                     // matrix, first row, rows of x in the tile, output tile
@@ -78,14 +88,30 @@ template <class T> __device__ __forceinline__ unsigned gm_idesc(int n)
     return (1u << 4) | (f << 7) | (f << 10) | ((unsigned)(n >> 3) << 17) | ((unsigned)(128 >> 4) << 24);
 }
 
-// 32 results of one output, one per row of x, from `at` on; results below `least` become it (ReLU: 0, else minus infinity).
+// 32 results of one output, one per row of x, from `at` on.
 template <class Y>
-__device__ __forceinline__ void gm_store(Y *at, long long ldy, int rows, const float (&v)[32], float least)
+__device__ __forceinline__ void gm_store(Y *at, long long ldy, int rows, const float (&v)[32])
 {
     #pragma unroll
     for (int c = 0; c < 32; c++) {
-        if (c < rows) *at = from_float<Y>(v[c] < least ? least : v[c]);
+        if (c < rows) *at = from_float<Y>(v[c]);
         at += ldy;
+    }
+}
+
+// The same in 16 bits for the 32 outputs of a warp, from y's `at` on for output 0: ROWS rows of 64 bytes at a time go
+// through the warp's shared memory, so that a thread stores 16 bytes.  `outs`: outputs that exist (a multiple of 8).
+template <class Y, int ROWS>
+__device__ __forceinline__ void gm_store_rows(Y *at, long long ldy, int rows, int outs, unsigned char *stage, int lane, const float (&v)[32])
+{
+    const int r = lane >> 2, piece = lane & 3;
+    #pragma unroll
+    for (int c0 = 0; c0 < 32; c0 += ROWS) {
+        #pragma unroll
+        for (int c = 0; c < ROWS; c++) *(Y *)(stage + c * 64 + lane * 2) = from_float<Y>(v[c0 + c]);
+        __syncwarp();
+        if (r < ROWS && c0 + r < rows && piece * 8 < outs) *(uint4 *)(at + (c0 + r) * ldy + piece * 8) = *(const uint4 *)(stage + lane * 16);
+        __syncwarp();
     }
 }
 
@@ -99,16 +125,15 @@ __device__ __forceinline__ void cluster_sync()
 template <class T, int GROUP, int COLS, int HALVES, bool SPLIT>
 __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ W4Args a, int slices)
 {
-    using Stage = GmStage<COLS, HALVES>;
+    using Stage = GmStage<GROUP, COLS, HALVES>;
     constexpr int STAGES = Stage::COUNT, BUFS = Stage::BUFFERS, GPT = W4_TILE / GROUP, ROWS = HALVES * COLS, CHUNKS = COLS / 64;
     constexpr unsigned HALF = Stage::HALF;
-    extern __shared__ unsigned char gm_smem[];
-    __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * GM_SLOTS + 2 * BUFS];
-    __shared__ unsigned tmem_slot;
-    __shared__ int tile_end[GM_MAX_E];                            // row tiles of the matrices up to and including this one
-    __shared__ int scan[16];
-    const unsigned smem = (s_addr(gm_smem) + 1023u) & ~1023u;
-    const unsigned full = s_addr(&bars[0]), empty = full + 8 * STAGES, a_full = empty + 8 * STAGES, a_empty = a_full + 8 * GM_SLOTS,
+    extern __shared__ __align__(1024) unsigned char gm_smem[];    // the swizzle pattern repeats every 1024 bytes
+    GmRest &rest = *(GmRest *)(gm_smem + Stage::REST);
+    int *tile_end = rest.tile_end, *scan = rest.scan;
+    unsigned &tmem_slot = rest.tmem_slot;
+    const unsigned smem = s_addr(gm_smem);
+    const unsigned full = s_addr(rest.bars), empty = full + 8 * STAGES, a_full = empty + 8 * STAGES, a_empty = a_full + 8 * GM_SLOTS,
                    d_full = a_empty + 8 * GM_SLOTS, d_empty = d_full + 8 * BUFS;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const W4Weights &w = a.w;
@@ -382,26 +407,36 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                                  "r"((unsigned)(tot[0][c >> 5][c >> 1 & 15] >> (32 * (c & 1)))) : "memory");
                 continue;
             }
-            if (!ok || n >= w.N) continue;
-            const float bias = a.bias ? a.bias[(size_t)t.e * w.N + n] : 0.f;
+            if (!ok) continue;
+            const float bias = a.bias && n < w.N ? a.bias[(size_t)t.e * w.N + n] : 0.f;
+            const int n0 = t.nt * W4_TILE + q4 * 32;                       // the warp's outputs
+            unsigned char *stage = gm_smem + Stage::STORE + (warp - 4) * Stage::STORE_ROWS * 64;
             #pragma unroll
             for (int h = 0; h < HALVES; h++)
                 #pragma unroll
                 for (int p = 0; p < CHUNKS; p++) {
                     const int row = h * COLS + part * (COLS / 2) + p * 32;
                     if (row >= t.rows) continue;
-                    const size_t at = (size_t)(t.row0 + row) * a.ldy + n;
+                    const int left = t.rows - row;
+                    const size_t at = (size_t)(t.row0 + row) * a.ldy + n0;
                     float v[32];
                     #pragma unroll
                     for (int c = 0; c < 32; c++) v[c] = __uint_as_float((unsigned)(tot[h][p][c >> 1] >> (32 * (c & 1)))) + bias;
-                    if (a.act == 2) {
+                    if (a.act == 1) {
+                        #pragma unroll
+                        for (int c = 0; c < 32; c++) v[c] = w4_act(v[c], 1);
+                    } else if (a.act == 2) {
                         #pragma unroll
                         for (int c = 0; c < 32; c++) v[c] = w4_act(v[c], 2);
                     }
-                    const float least = a.act == 1 ? 0.f : __int_as_float(0xff800000);
-                    if (a.y_dtype == BLS_F32) gm_store((float *)a.y + at, a.ldy, t.rows - row, v, least);
-                    else if (a.y_dtype == BLS_BF16) gm_store((__nv_bfloat16 *)a.y + at, a.ldy, t.rows - row, v, least);
-                    else gm_store((__half *)a.y + at, a.ldy, t.rows - row, v, least);
+                    if (a.y_pieces) {
+                        if (a.y_dtype == BLS_BF16) gm_store_rows<__nv_bfloat16, Stage::STORE_ROWS>((__nv_bfloat16 *)a.y + at, a.ldy, left, w.N - n0, stage, lane, v);
+                        else gm_store_rows<__half, Stage::STORE_ROWS>((__half *)a.y + at, a.ldy, left, w.N - n0, stage, lane, v);
+                    } else if (n < w.N) {
+                        if (a.y_dtype == BLS_F32) gm_store((float *)a.y + at + lane, a.ldy, left, v);
+                        else if (a.y_dtype == BLS_BF16) gm_store((__nv_bfloat16 *)a.y + at + lane, a.ldy, left, v);
+                        else gm_store((__half *)a.y + at + lane, a.ldy, left, v);
+                    }
                 }
         }
         if (SPLIT) {
@@ -478,7 +513,7 @@ cudaError_t launch_tiles_h(const W4Args &a, int grid, int slices, cudaStream_t s
 {
     CUtensorMap map;
     if (!tc_make_map(&map, a.x, a.rows, a.w.K, a.ldx, COLS)) return cudaErrorInvalidValue;
-    const size_t smem = 1024 + (size_t)GmStage<COLS, HALVES>::ALL;
+    const size_t smem = GmStage<GROUP, COLS, HALVES>::ALL;
     auto kernel = bls_w4_tiles_kernel<T, GROUP, COLS, HALVES, SPLIT>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
