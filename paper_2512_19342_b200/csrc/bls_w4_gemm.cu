@@ -21,13 +21,13 @@
 
 namespace {
 
-constexpr int GM_SLOTS = 4;                                   // tensor-memory slots of unpacked weights
+constexpr int GM_SLOTS = 2;                                   // tensor-memory slots of unpacked weights
 constexpr int GM_THREADS = 16 * 32;                           // warps 14 and 15 only fill the fourth warpgroup
-constexpr unsigned GM_TMEM_COLS = 512, GM_A_COL = 256;        // accumulators: columns 0..255; weights: 4 x 64 columns
+constexpr unsigned GM_TMEM_COLS = 512, GM_A_COL = GM_TMEM_COLS - GM_SLOTS * 64;       // accumulators, then the weights' slots of 64 columns
 constexpr int GM_MAX_E = 1024;
 
 struct GmRest {
-    unsigned long long bars[2 * 8 + 2 * GM_SLOTS + 2 * 4];        // at most 8 stages and 4 accumulators
+    unsigned long long bars[2 * 8 + 2 * GM_SLOTS + 2 * 6];        // at most 8 stages and 6 accumulators
     int tile_end[GM_MAX_E];                                       // row tiles of the matrices up to and including this one
     int scan[16];
     unsigned tmem_slot;
@@ -38,7 +38,7 @@ struct GmRest {
 // and more of them have to be under way.  A stage of 128 inputs: x, the weight tile, the scales and the zero points of its groups.
 template <int GROUP, int COLS, int HALVES> struct GmStage {
     static constexpr int COUNT = HALVES == 2 ? 3 : COLS == 128 ? 5 : 8;                                     // what fits into 227 KB
-    static constexpr int BUFFERS = HALVES == 2 ? 2 : 256 / COLS;
+    static constexpr int BUFFERS = GM_A_COL / COLS;
     static constexpr unsigned HALF = COLS * W4_TILE * 2, W = HALVES * HALF, BYTES = W + W4_TILE_BYTES;      // x (two boxes of 64 inputs), weights
     // after all stages: scales and zero points, 64-byte rows of results for each of the eight storing warps, and the rest
     static constexpr int GPT = W4_TILE / GROUP, STORE_ROWS = HALVES == 2 && GROUP == 32 ? 4 : 8;
@@ -63,6 +63,22 @@ __device__ __forceinline__ void tmem_st16(unsigned taddr, const unsigned (&r)[16
                  "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
                  ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
                    "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+}
+// 16 columns of this warp's lanes; the registers hold them after tmem_wait_ld().
+__device__ __forceinline__ void tmem_ld16(unsigned taddr, unsigned (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr) : "memory");
+}
+// The registers pass through, so that nothing that uses them is moved before the wait.
+__device__ __forceinline__ void tmem_wait_ld(unsigned (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
 }
 __device__ __forceinline__ bool elect_one()
 {
@@ -248,7 +264,7 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         } else if (warp == 13) {
             // the whole warp follows, one thread of it issues
             const bool leader = elect_one();
-            unsigned s = 0, ph = 0, j = 0, jph = 0, used[2] = {0, 0}, b = 0;
+            unsigned s = 0, ph = 0, j = 0, jph = 0, used = 0, b = 0;                  // used: how often all accumulators have been filled
             bool ok = true;
             for (int i = first_tile; i < tiles && ok; i += step) {
                 const GmTile t = tile_of(i);
@@ -263,9 +279,7 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                         for (int h = 0; h < HALVES; h++) {
                             const int rows = min(COLS, t.rows - h * COLS);
                             if (rows <= 0) continue;
-                            if (HALVES == 2) b = h;
-                            ok = ok && mb_wait(d_empty + 8 * b, (used[HALVES == 2 ? h : 0] & 1) ^ 1, a.status);
-                            if (HALVES == 2 || b == BUFS - 1) used[HALVES == 2 ? h : 0]++;    // how often the buffer (HALVES == 1: all) has been filled
+                            ok = ok && mb_wait(d_empty + 8 * b, (used & 1) ^ 1, a.status);
                             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                             if (leader && ok) {
                                 const unsigned idesc = gm_idesc<T>((rows + 15) & ~15);
@@ -277,7 +291,7 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                                 }
                                 umma_commit(d_full + 8 * b);
                             }
-                            if (HALVES == 1) b = b == BUFS - 1 ? 0 : b + 1;
+                            if (++b == BUFS) { b = 0; used++; }
                         }
                     }
                     if (leader && ok) {
@@ -346,7 +360,7 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         // scale and store: thread = output, half of the rows of x of every half of the tile
         const int q4 = warp & 3, part = (warp - 4) >> 2, r = q4 * 32 + lane;
         const unsigned lanes = (unsigned)(q4 * 32) << 16;
-        unsigned s = 0, ph = 0, used[2] = {0, 0}, b = 0;
+        unsigned s = 0, ph = 0, used = 0, b = 0;
         bool ok = true;
         for (int i = first_tile; i < tiles && ok; i += step) {
             const GmTile t = tile_of(i);
@@ -371,29 +385,30 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
                     #pragma unroll
                     for (int h = 0; h < HALVES; h++) {
                         if (h * COLS >= t.rows) continue;
-                        if (HALVES == 2) b = h;
-                        ok = ok && mb_wait(d_full + 8 * b, used[HALVES == 2 ? h : 0] & 1, a.status);
-                        if (HALVES == 2 || b == BUFS - 1) used[HALVES == 2 ? h : 0]++;
+                        ok = ok && mb_wait(d_full + 8 * b, used & 1, a.status);
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         const bool busy = ok && h * COLS + part * (COLS / 2) < t.rows;     // the whole warp alike
                         const unsigned src = tmem + lanes + b * COLS + part * (COLS / 2);
-                        unsigned v[32];
+                        // all of this thread's columns are read at once, so that the accumulator is free as early as possible
+                        constexpr int PARTS = COLS / 32;
+                        unsigned v[PARTS][16];
                         if (busy) {
-                            tmem_ld32(src, v);
-                            if (CHUNKS == 2) {
-                                #pragma unroll
-                                for (int c = 0; c < 16; c++) tot[h][0][c] = fma2(s2, v[2 * c], v[2 * c + 1], tot[h][0][c]);
-                                tmem_ld32(src + 32, v);
-                            }
+                            #pragma unroll
+                            for (int p = 0; p < PARTS; p++) tmem_ld16(src + p * 16, v[p]);
+                            #pragma unroll
+                            for (int p = 0; p < PARTS; p++) tmem_wait_ld(v[p]);
                         }
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                         __syncwarp();
                         if (lane == 0) mb_arrive(d_empty + 8 * b);
                         if (busy) {
                             #pragma unroll
-                            for (int c = 0; c < 16; c++) tot[h][CHUNKS - 1][c] = fma2(s2, v[2 * c], v[2 * c + 1], tot[h][CHUNKS - 1][c]);
+                            for (int p = 0; p < PARTS; p++)
+                                #pragma unroll
+                                for (int c = 0; c < 8; c++)
+                                    tot[h][p >> 1][(p & 1) * 8 + c] = fma2(s2, v[p][2 * c], v[p][2 * c + 1], tot[h][p >> 1][(p & 1) * 8 + c]);
                         }
-                        if (HALVES == 1) b = b == BUFS - 1 ? 0 : b + 1;
+                        if (++b == BUFS) { b = 0; used++; }
                     }
                 }
                 if (++s == STAGES) { s = 0; ph ^= 1; }
