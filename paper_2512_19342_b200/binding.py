@@ -495,10 +495,10 @@ def _rows(t: torch.Tensor, name: str, shape: tuple, dtype: torch.dtype):
     """(address, row pitch) of a matrix of one type on a GPU whose rows are contiguous, at any pitch."""
     if t.is_cuda and t.dtype is dtype and t.shape == shape:
         ld, step = t.stride()
-        if shape[0] < 2:
-            ld = max(shape[1], 1)
-        if (step == 1 or shape[1] < 2) and ld >= shape[1]:
-            return t.data_ptr(), max(ld, 1)
+        if step == 1 and ld >= shape[1] > 0:
+            return t.data_ptr(), ld
+        if (step == 1 or shape[1] < 2) and (ld >= shape[1] or shape[0] < 2):     # one row or column: its strides say nothing
+            return t.data_ptr(), max(ld, shape[1], 1)
     raise ValueError(f"{name}: expected a CUDA matrix {shape} of {dtype} with contiguous rows, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}, on {t.device}")
 
 
@@ -593,9 +593,13 @@ class W4:
             raise ValueError("W4: bad sizes")
         nt, kt, E = (N + 127) // 128, (K + 127) // 128, q.shape[0]
         shape = (E, kt * 128 // group, nt * 128)
-        self._args = (_flat(q, "q", (E, nt, kt, 128, 64), torch.uint8), _flat(scale, "scale", shape, torch.bfloat16),
-                      _flat(zero, "zero", shape, torch.uint8), E, N, K, group)
+        self._set(_flat(q, "q", (E, nt, kt, 128, 64), torch.uint8), _flat(scale, "scale", shape, torch.bfloat16),
+                  _flat(zero, "zero", shape, torch.uint8), q, scale, zero, E, N, K, group)
+
+    def _set(self, pq, ps, pz, q, scale, zero, E, N, K, group):
+        self._args = (pq, ps, pz, E, N, K, group)
         self.q, self.scale, self.zero, self.E, self.N, self.K, self.group = q, scale, zero, E, N, K, group
+        return self
 
 
 def bls_w4_sizes(E: int, N: int, K: int, group: int):
@@ -607,8 +611,12 @@ def bls_w4_sizes(E: int, N: int, K: int, group: int):
 
 def _matrices(w: torch.Tensor, name: str):
     """(E, N, K, row pitch) of weights [E][N][K] or [N][K] with contiguous rows, matrices N pitches apart."""
-    _need(w.is_cuda and w.dtype in _DTYPE and w.dim() in (2, 3) and w.numel() > 0, f"{name}: expected CUDA weights [N][K] or [E][N][K]")
-    E, (N, K) = (w.shape[0] if w.dim() == 3 else 1), w.shape[-2:]
+    shape = w.shape
+    if not (w.is_cuda and w.dtype in _DTYPE and len(shape) in (2, 3) and w.numel() > 0):
+        raise ValueError(f"{name}: expected CUDA weights [N][K] or [E][N][K], got {tuple(shape)} of {w.dtype} on {w.device}")
+    E, N, K = shape if len(shape) == 3 else (1, *shape)
+    if w.is_contiguous():
+        return E, N, K, K
     ld = w.stride(-2) if N > 1 else (w.stride(0) if E > 1 else K)
     _need((K < 2 or w.stride(-1) == 1) and ld >= K and (E < 2 or w.stride(0) == N * ld), f"{name}: rows must be contiguous, matrices N rows apart")
     return E, N, K, ld
@@ -623,16 +631,21 @@ def bls_w4_quantize(w: torch.Tensor, group: int = 128, symmetric: bool = True, s
     with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():      # memory of the call's own stream
         q, scale = w.new_empty((E, nt, kt, 128, 64), dtype=torch.uint8), w.new_empty(shape, dtype=torch.bfloat16)
         zero = None if symmetric else w.new_empty(shape, dtype=torch.uint8)
-    t = W4(q, scale, zero, N, K, group)
-    _check(lib().bls_w4_quantize(w.data_ptr(), _DTYPE[w.dtype], ld, E, N, K, group, *t._args[:3], _on(stream, w)), "bls_w4_quantize")
-    return t
+    pq, ps, pz = q.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr()
+    code = lib().bls_w4_quantize(w.data_ptr(), _DTYPE[w.dtype], ld, E, N, K, group, pq, ps, pz, _on(stream, w))
+    if code:
+        raise BlsError(code, "bls_w4_quantize")
+    return W4.__new__(W4)._set(pq, ps, pz, q, scale, zero, E, N, K, group)
 
 
 def bls_w4_dequantize(w4: W4, w: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """w [E][N][K] (or [N][K] with E = 1) = (q - z) * s, rounded once to w's type."""
     E, N, K, ld = _matrices(w, "w")
-    _need((E, N, K) == (w4.E, w4.N, w4.K), f"w: expected {(w4.E, w4.N, w4.K)}")
-    _check(lib().bls_w4_dequantize(*w4._args, w.data_ptr(), _DTYPE[w.dtype], ld, _on(stream, w)), "bls_w4_dequantize")
+    if (E, N, K) != (w4.E, w4.N, w4.K):
+        raise ValueError(f"w: expected {(w4.E, w4.N, w4.K)}")
+    code = lib().bls_w4_dequantize(*w4._args, w.data_ptr(), _DTYPE[w.dtype], ld, _on(stream, w))
+    if code:
+        raise BlsError(code, "bls_w4_dequantize")
 
 
 _w4_status_word = {}                         # device number -> (int32 [1], its address), zeroed once: waits that gave up are latched here
