@@ -457,11 +457,11 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         if (SPLIT) {
             cluster_sync();
             if (first_tile < tiles) {
-                // every CTA finishes 128 / slices outputs (slices is a power of two)
+                // four outputs at a time: every CTA finishes its share of the 32 fours of a row
                 const GmTile t = tile_of(first_tile);
-                const int shift = 5 - (31 - __clz(slices));                // four outputs at a time
-                for (int i = threadIdx.x - 128; i < t.rows << shift; i += 256) {
-                    const int row = i >> shift, o = ((rank << shift) + (i & ((1 << shift) - 1))) * 4, n = t.nt * W4_TILE + o;
+                const int four0 = 32 * rank / slices, fours = 32 * (rank + 1) / slices - four0;
+                for (int i = threadIdx.x - 128; i < t.rows * fours; i += 256) {
+                    const int row = i / fours, o = (four0 + i % fours) * 4, n = t.nt * W4_TILE + o;
                     const unsigned at = smem + (row * W4_TILE + o) * 4;
                     float p[8][4], v[4] = {0.f, 0.f, 0.f, 0.f};
                     #pragma unroll
@@ -539,8 +539,7 @@ cudaError_t launch_tiles_h(const W4Args &a, int grid, int slices, cudaStream_t s
 template <class T, int GROUP, int COLS>
 cudaError_t launch_tiles_c(const W4Args &a, long long tiles, cudaStream_t s)
 {
-    int slices = 1;
-    while (slices < 8 && tiles * slices * 2 <= sm_count() && slices * 4 <= a.w.KT) slices *= 2;
+    const int slices = (int)max(1ll, min(min(8ll, sm_count() / tiles), a.w.KT / 2ll));
     if (slices > 1) return launch_tiles_h<T, GROUP, COLS, 1, true>(a, (int)tiles * slices, slices, s);
     return launch_tiles_h<T, GROUP, COLS, 1, false>(a, (int)min(tiles, (long long)sm_count()), 1, s);
 }
