@@ -240,8 +240,8 @@ __device__ __forceinline__ void w4_floats(const W4Raw<__half> &r, float (&v)[8])
     }
 }
 
-// grid (KT, NT, E): one tile.  A lane takes the eight inputs of one stored word, half a warp an output row; a
-// group is 4, 8 or 16 neighbouring lanes.  A thread asks for four rows' pieces before it uses the
+// grid (KT, NT, E): one tile.  A lane takes the sixteen inputs of two stored words, eight lanes an output row; a
+// group is 2, 4 or 8 neighbouring lanes.  A thread asks for two rows' pieces before it uses the
 // first.  WHOLE: rows of w start at 16-byte boundaries.
 //
 // The floor is reading w once, which leaves about 20 instructions per element.  So rint(w / s) of the
@@ -260,30 +260,34 @@ __global__ void __launch_bounds__(256) bls_w4_quantize_kernel(const void *wv, lo
     __shared__ __nv_bfloat16 s_sc[4][W4_TILE];
     __shared__ uint8_t s_z[4][W4_TILE];
     const int kt = blockIdx.x, nt = blockIdx.y, e = blockIdx.z;
-    const int l = threadIdx.x & 15;
-    const int gpt = W4_TILE / d.group, lanes = d.group / 8;
-    const int k = kt * W4_TILE + l * 8;
+    const int l = threadIdx.x & 7;
+    const int gpt = W4_TILE / d.group, lanes = d.group / 16;
+    const int k = kt * W4_TILE + l * 16;
     const T *w = (const T *)wv + ((size_t)e * d.N + nt * W4_TILE) * ldw + k;
     uint8_t *tile = q + (((size_t)e * d.NT + nt) * d.KT + kt) * W4_TILE_BYTES;
     #pragma unroll 1
-    for (int r0 = threadIdx.x >> 4; r0 < W4_TILE; r0 += 64) {
-        W4Raw<T> p[4];
+    for (int r0 = threadIdx.x >> 3; r0 < W4_TILE; r0 += 64) {
+        W4Raw<T> p[2][2];
         #pragma unroll
-        for (int u = 0; u < 4; u++) {
-            const int r = r0 + u * 16;
-            p[u] = w4_load8<T, WHOLE>(w + r * ldw, nt * W4_TILE + r < d.N ? d.K - k : 0);
+        for (int u = 0; u < 2; u++) {
+            const int r = r0 + u * 32, avail = nt * W4_TILE + r < d.N ? d.K - k : 0;
+            p[u][0] = w4_load8<T, WHOLE>(w + r * ldw, avail);
+            p[u][1] = w4_load8<T, WHOLE>(w + r * ldw + 8, avail - 8);
         }
         #pragma unroll
-        for (int u = 0; u < 4; u++) {
-            const int r = r0 + u * 16;
-            float v[8], lo = 0.f, hi = 0.f, bad = 0.f;                       // bad: NaN after a value that is not finite
-            w4_floats(p[u], v);
+        for (int u = 0; u < 2; u++) {
+            const int r = r0 + u * 32;
+            float v[2][8], lo = 0.f, hi = 0.f, bad = 0.f;                       // bad: NaN after a value that is not finite
+            w4_floats(p[u][0], v[0]);
+            w4_floats(p[u][1], v[1]);
             #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                bad = fmaf(v[i], 0.f, bad);
-                if (ZERO) lo = fminf(lo, v[i]);
-                hi = fmaxf(hi, ZERO ? v[i] : fabsf(v[i]));
-            }
+            for (int j = 0; j < 2; j++)
+                #pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    bad = fmaf(v[j][i], 0.f, bad);
+                    if (ZERO) lo = fminf(lo, v[j][i]);
+                    hi = fmaxf(hi, ZERO ? v[j][i] : fabsf(v[j][i]));
+                }
             if (bad != 0.f) hi = __int_as_float(0x7f800000);
             for (int o = 1; o < lanes; o <<= 1) {
                 if (ZERO) lo = fminf(lo, __shfl_xor_sync(~0u, lo, o));
@@ -299,25 +303,36 @@ __global__ void __launch_bounds__(256) bls_w4_quantize_kernel(const void *wv, lo
             const float below = inv * (1.f - 0x1p-19f), above = inv * (1.f + 0x1p-19f);
             constexpr float ROUND = 12582912.f;                              // 1.5 2^23
             constexpr unsigned BITS = 0x4b400000u;                           // its bits
-            unsigned word = (unsigned)z * 0x11111111u - BITS * 0x11111111u, differ = 0;
+            unsigned word[2], differ = 0;
             #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                unsigned t = __float_as_uint(fmaf(v[i], below, ROUND));
-                const unsigned t2 = __float_as_uint(fmaf(v[i], above, ROUND));
-                if (DT == BLS_F32) differ |= t ^ t2;
-                else if (t & 1) t = t2;
-                if (ZERO) t = min(t, BITS + 15u - z);                        // rint(w / s) + z is at least 0, but can reach 16
-                word += t << (4 * ((i >> 1) + 4 * (i & 1)));
-            }
-            if (differ || !(fmaxf(hi, -lo) * inv < (ZERO ? 15.5f : 7.5f))) {      // !(..): also where inv is NaN
-                word = 0;
+            for (int j = 0; j < 2; j++) {
+                word[j] = (unsigned)z * 0x11111111u - BITS * 0x11111111u;
                 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    const int c = usable ? (int)rintf(__fdiv_rn(v[i], s)) : 0;
-                    word |= (unsigned)min(max(c + z, 0), 15) << (4 * ((i >> 1) + 4 * (i & 1)));
+                    unsigned t = __float_as_uint(fmaf(v[j][i], below, ROUND));
+                    const unsigned t2 = __float_as_uint(fmaf(v[j][i], above, ROUND));
+                    if (DT == BLS_F32) differ |= t ^ t2;
+                    else if (t & 1) t = t2;
+                    if (ZERO) t = min(t, BITS + 15u - z);                    // rint(w / s) + z is at least 0, but can reach 16
+                    word[j] += t << (4 * ((i >> 1) + 4 * (i & 1)));
                 }
             }
-            *(unsigned *)(tile + r * 64 + ((l & 3) ^ ((r >> 1) & 3)) * 16 + (l >> 2) * 4) = word;
+            if (differ || !(fmaxf(hi, -lo) * inv < (ZERO ? 15.5f : 7.5f))) {      // !(..): also where inv is NaN
+                #pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    word[j] = 0;
+                    #pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const int c = usable ? (int)rintf(__fdiv_rn(v[j][i], s)) : 0;
+                        word[j] |= (unsigned)min(max(c + z, 0), 15) << (4 * ((i >> 1) + 4 * (i & 1)));
+                    }
+                }
+            }
+            #pragma unroll
+            for (int j = 0; j < 2; j++) {
+                const int m = 2 * l + j;                                     // eight inputs: block m / 4 of 32, quarter m mod 4
+                *(unsigned *)(tile + r * 64 + ((m & 3) ^ ((r >> 1) & 3)) * 16 + (m >> 2) * 4) = word[j];
+            }
             if (l % lanes == 0) {
                 s_sc[l / lanes][r] = sb;
                 s_z[l / lanes][r] = (uint8_t)z;
