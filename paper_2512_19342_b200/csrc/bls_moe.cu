@@ -4,7 +4,7 @@
 // Routing is a stable counting sort.  A tile of consecutive slots is counted per warp, an
 // exclusive scan over (expert, tile, warp) gives every warp its first position for every
 // expert, and inside a warp the position of a slot is the number of lower lanes with the same
-// expert (match.any).  Up to ROUTE_ONE slots one block does it all; more take a kernel that counts
+// expert.  Up to ROUTE_ONE slots one block does it all; more take a kernel that counts
 // the tiles and one in which every block adds up the counts before its own (tiles x E integers
 // from L2) and sorts its tile.  Positions depend on scans only: the result is the unique stable sort, the
 // same in every run.
@@ -47,6 +47,19 @@ __device__ __forceinline__ int block_scan(int v, int *scratch)
     return v + (warp ? scratch[warp - 1] : 0);
 }
 
+// The lanes whose expert is this lane's, found bit by bit: 1 + log2(E) votes, a few instructions each (the warp's match instruction
+// takes a turn for every different value, 400 cycles for 32 random experts).
+__device__ __forceinline__ unsigned same_expert(int e, int bits)
+{
+    unsigned same = ~0u;
+    for (int b = 0; b < bits; b++) {
+        const bool set = (e >> b) & 1;
+        const unsigned v = __ballot_sync(~0u, set);
+        same &= set ? v : ~v;
+    }
+    return same;
+}
+
 // Counts of a tile's experts: row blockIdx.x of count [tiles][E].
 __global__ void __launch_bounds__(ROUTE_THREADS) bls_moe_count_kernel(const int *expert, int n, int E, int tile, int *count)
 {
@@ -81,12 +94,10 @@ __global__ void __launch_bounds__(ROUTE_THREADS) bls_moe_route_kernel(const int 
     const int per = ((t1 - t0 + ROUTE_WARPS - 1) / ROUTE_WARPS + 31) & ~31;   // consecutive slots of a warp
     const int lo = min(t0 + warp * per, t1), hi = min(lo + per, t1);
     int *mine = hist + warp * E;
+    const int bits = 32 - __clz(E);
     for (int i = lo; i < hi; i += 32) {
         const int e = i + lane < hi ? expert[i + lane] : -1;
-        const bool kept = (unsigned)e < (unsigned)E;
-        const unsigned same = __match_any_sync(~0u, kept ? e : -1);
-        if (kept && lane == __ffs(same) - 1) mine[e] += __popc(same);
-        __syncwarp();
+        if ((unsigned)e < (unsigned)E) atomicAdd(&mine[e], 1);
     }
     if (TILED) {
         // every thread adds up one expert over a part of the tiles
@@ -128,7 +139,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) bls_moe_route_kernel(const int 
     for (int i = lo; i < hi; i += 32) {
         const int e = i + lane < hi ? expert[i + lane] : -1;
         const bool kept = (unsigned)e < (unsigned)E;
-        const unsigned same = __match_any_sync(~0u, kept ? e : -1);
+        const unsigned same = same_expert(kept ? e : E, bits);
         const int first = kept ? mine[e] : 0;
         __syncwarp();
         if (kept) {
@@ -145,11 +156,13 @@ __global__ void __launch_bounds__(ROUTE_THREADS) bls_moe_route_kernel(const int 
     for (int i = max(t0, scratch[31]) + threadIdx.x; i < t1; i += ROUTE_THREADS) order[i] = -1;
 }
 
-// Tiles of the slots: as many as there are SMs, of 1024 slots at least; one tile up to ROUTE_ONE slots.
+// Tiles of the slots, of 1024 slots at least; one up to ROUTE_ONE slots (one block and one launch: 4000 slots take 6.4 us, two
+// kernels 5.4 us and another launch; 8000 slots 10.3 and 5.4).  74 tiles, half the SMs: every block reads the counts of all tiles, and
+// 400k slots over 256 experts take 13.7 us with 74 tiles, 18.3 with 148, 16.1 with 50.
 void route_tiles(long long n, int &tiles, int &tile)
 {
     if (n <= ROUTE_ONE) { tiles = 1; tile = (int)n; return; }
-    const long long want = min((n + 1023) / 1024, 148ll);
+    const long long want = min((n + 1023) / 1024, 74ll);
     tile = (int)(((n + want - 1) / want + 31) & ~31ll);
     tiles = (int)((n + tile - 1) / tile);
 }

@@ -410,7 +410,8 @@ bool w4_shape(int E, int N, int K, int group, W4Weights &w)
     return true;
 }
 
-// Which kernel: by the rows that a matrix gets on average.
+// Which kernel: by the rows that a matrix gets on average.  4096 x 4096: 8 rows 6.9 us here, 9 rows 9.4 us in tiles and 10.2 here,
+// 16 rows 9.5 and 11.6; 8192 x 8192: 8 rows 20 us here, 16 rows 20 in tiles and 38 here.
 bool many_rows(const W4Weights &w, int64_t rows) { return rows > 8ll * w.E; }
 
 template <class T, int GROUP>
