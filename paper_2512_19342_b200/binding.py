@@ -672,7 +672,7 @@ def bls_w4_linear(w4: W4, x: torch.Tensor, y: torch.Tensor, offsets: Optional[to
                   bias: Optional[torch.Tensor] = None, act: int = 0, stream: Optional[torch.cuda.Stream] = None) -> None:
     """y = act(x W^T + bias), row by row with the matrix that offsets int32 [E+1] gives it (None with E = 1); rows from
     offsets[-1] on become 0.  x [rows][K] bf16 or f16, y [rows][N] bf16, f16 or fp32, bias fp32 [E][N];
-    act 0 none, 1 ReLU, 2 logistic function."""
+    act 0 none, 1 ReLU, 2 logistic function.  The first call on a device sets up its status word and synchronises: make it before any capture."""
     E, N, K = w4.E, w4.N, w4.K
     rows = _two(x, "x")[0]
     if x.dtype is _F32 or (offsets is None and E != 1):

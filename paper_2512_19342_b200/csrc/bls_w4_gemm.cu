@@ -201,9 +201,8 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         __syncthreads();
     }
     if (a.offsets) {                                               // rows of no matrix become 0
-        const int first = min(max(a.offsets[w.E], 0), a.rows);
-        for (long long i = (long long)blockIdx.x * GM_THREADS + threadIdx.x; i < (long long)(a.rows - first) * w.N; i += (long long)gridDim.x * GM_THREADS)
-            w4_store(a.y, (size_t)(first + i / w.N) * a.ldy + i % w.N, a.y_dtype, 0.f);
+        for (int row = min(max(a.offsets[w.E], 0), a.rows) + blockIdx.x; row < a.rows; row += gridDim.x)
+            for (int n = threadIdx.x; n < w.N; n += GM_THREADS) w4_store(a.y, (size_t)row * a.ldy + n, a.y_dtype, 0.f);
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
