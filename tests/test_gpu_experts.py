@@ -618,3 +618,48 @@ def test_linear_by_experts_of_many_rows():
     bias = torch.randn(E, N, device="cuda", generator=g)
     check_linear(t, w, x, offsets, bias, 0, BF16)
     check_linear(t, w, x, offsets, bias, 2, F32)
+
+
+@pytest.mark.parametrize("rows", [5, 8, 20, 150])
+def test_linear_of_one_matrix_with_offsets_and_of_long_rows(rows):
+    """One matrix that answers a part of the rows; K of several turns of a block's warps, and of slices of unequal length."""
+    g = gen("one", rows)
+    for K, N in ((200, 136), (5000, 90), (4224, 264)):
+        t, w = weights(g, 1, N, K, 32, False)
+        x = torch.randn(rows, K, device="cuda", generator=g).to(BF16)
+        for live in (0, 1, rows - 1, rows):
+            off = torch.tensor([0, live], dtype=torch.int32, device="cuda")
+            check_linear(t, w, x, off, torch.randn(1, N, device="cuda", generator=g), 1, BF16)
+        check_linear(t, w, x, None, None, 0, F32)
+
+
+@pytest.mark.parametrize("rows", [3, 40, 1500, 9000])
+def test_linear_by_a_thousand_experts(rows):
+    """More matrices than rows (the ones that have rows are looked up), and more than a block has threads."""
+    E, N, K = 1024, 24, 64
+    g = gen("thousand", rows)
+    t, w = weights(g, E, N, K, 64, True)
+    e = torch.sort(torch.randint(0, E, (rows,), device="cuda", generator=g)).values
+    offsets = torch.searchsorted(e, torch.arange(E + 1, device="cuda")).to(torch.int32)
+    x = torch.randn(rows, K, device="cuda", generator=g).to(F16)
+    y = torch.empty(rows, N, device="cuda")
+    bls.bls_w4_linear(t, x, y, offsets=offsets)
+    assert bls.bls_w4_status() == bls.BLS_OK
+    want = torch.einsum("rk,rnk->rn", x.double(), w[e])
+    size = torch.einsum("rk,rnk->rn", x.double().abs(), w[e].abs())
+    close(y, want, size, 2 * K + 13)
+
+
+def test_offsets_outside_the_rows_are_cut():
+    """A broken offsets array (negative, past the rows, falling) cannot lead outside x and y: whatever rows it names, the guard rows
+    after y stay untouched."""
+    g = gen("broken")
+    t, _ = weights(g, 4, 72, 96, 32, True)
+    for rows in (6, 300):
+        x = torch.randn(rows, 96, device="cuda", generator=g).to(BF16)
+        buf = torch.full((rows + 8, 72), 7.0, device="cuda", dtype=BF16)
+        for off in ([-5, 2, 3, 4, rows], [0, rows + 50, rows + 60, 3, 5], [4, 3, 2, 1, 0], [0, 0, 0, 0, 2 ** 31 - 1]):
+            bls.bls_w4_linear(t, x, buf[:rows], offsets=torch.tensor(off, dtype=torch.int32, device="cuda"))
+        torch.cuda.synchronize()
+        assert torch.all(buf[rows:] == 7.0)
+    assert bls.bls_w4_status() == bls.BLS_OK
