@@ -4,7 +4,7 @@
 // shared memory into tensor memory (integers q - z, exact in bf16 and f16), the rows of x are the
 // N operand in shared memory.  The accumulator of one group of inputs is complete after group / 16
 // instructions; it is then read back, scaled in fp32 and added to the running sums in registers,
-// while the next one (the other half of the rows, or the next group) accumulates in a second buffer.
+// while the next one (the other half of the rows, or the next group) accumulates in another buffer.
 // Weights are therefore never rounded, and a thread needs one scale per group, because its
 // accumulator lane is one output.
 //
@@ -37,7 +37,7 @@ struct GmRest {
 };
 
 // A tile has HALVES times COLS rows of x, COLS being the rows per product instruction (its N).  With one half of
-// 128 rows there are two accumulators, with one of 64 there are four: few rows make short products,
+// 128 rows there are three accumulators, with one of 64 there are six: few rows make short products,
 // and more of them have to be under way.  A stage of 128 inputs: x, the weight tile, the scales and the zero points of its groups.
 template <int GROUP, int COLS, int HALVES> struct GmStage {
     static constexpr int COUNT = HALVES == 2 ? 3 : COLS == 128 ? 5 : 8;                                     // what fits into 227 KB
