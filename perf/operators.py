@@ -116,6 +116,14 @@ def _plain_route(expert, E):
     return order, place, offsets
 
 
+def _scale(span, steps):
+    """span / steps (64 bits) rounded once to bfloat16's 8 bits, ties to even.  A division by a Python number would be a product with its
+    fp32 reciprocal on the GPU, and .to(bfloat16) from 64 bits rounds to 32 bits in between; both are off where the quotient is next to a tie."""
+    bits = (span / torch.full_like(span, steps)).view(torch.int64)
+    bits = (bits + ((1 << 44) - 1) + (bits >> 45 & 1)) & -(1 << 45)                     # 52 - 7 bits go
+    return bits.view(torch.float64).to(torch.bfloat16)
+
+
 def _quantize(w, group, zero):
     """w [E][N][K] of any type -> whole numbers 0..15 float32 [E][N][Kp], scale bf16 and zero float32 [E][N][groups]; K padded to 128."""
     E, N, K = w.shape
@@ -123,12 +131,12 @@ def _quantize(w, group, zero):
     g = torch.nn.functional.pad(w.float(), (0, Kp - K)).reshape(E, N, Kp // group, group)
     if zero:
         lo, hi = g.amin(3).clamp(max=0), g.amax(3).clamp(min=0)
-        scale = ((hi - lo) / 15.0).to(torch.bfloat16)
+        scale = _scale(hi.double() - lo.double(), 15.0)
         s = scale.float()
         z = torch.where(s > 0, (-lo / s).round(), 0.0).clamp(0, 15)
         q = torch.where(s[..., None] > 0, (g / s[..., None]).round(), 0.0)
     else:
-        scale = (g.abs().amax(3) / 7.0).to(torch.bfloat16)
+        scale = _scale(g.abs().amax(3).double(), 7.0)
         s = scale.float()
         z = torch.full_like(s, 8.0)
         q = torch.where(s[..., None] > 0, (g / s[..., None]).round(), 0.0)
