@@ -418,7 +418,7 @@ bls_status_t bls_moe_combine_grad(const void *dout, int64_t ldd, const void *y, 
  *                      With zero points, lo = min(w, 0), hi = max(w, 0): s = bf16((hi - lo) / 15),
  *                      z = clamp(rint(-lo / s), 0, 15), q = clamp(rint(w / s) + z, 0, 15).  s = 0 gives
  *                      q = z; a NaN or an infinity (or s past bfloat16's range)
- *                      makes its whole group NaN.  Quotients are fp32.
+ *                      makes its whole group NaN.  s is the exact quotient rounded once; the quotients by s are fp32.
  *   bls_w4_dequantize  the weights (q - z) * s in fp32, rounded once to dtype
  *   bls_w4_bytes       workspace of bls_w4_linear for these x, ldx and rows (256-byte aligned; 0 up to
  *                      8 rows, and when rows of x start at 16-byte boundaries)

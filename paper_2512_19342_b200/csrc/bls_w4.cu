@@ -242,6 +242,27 @@ __device__ __forceinline__ void w4_floats(const W4Raw<__half> &r, float (&v)[8])
     }
 }
 
+// (span + more) / STEPS rounded once to bfloat16; more: what the rounded span leaves out.  A tie of bfloat16 times STEPS has few
+// enough bits for fp32, so the span and the quotient are rounded to one side of a tie or onto it, never past it.
+// On a tie the remainder, exact in fp32, says on which side the quotient lies, and the low bit of the fp32 quotient keeps it there.
+template <int STEPS>
+__device__ __forceinline__ float w4_scale(float span, float more)
+{
+    unsigned s = __float_as_uint(__fdiv_rn(span, (float)STEPS));
+    if ((s & 0xffffu) == 0x8000u) {
+        float rest = fmaf(-(float)STEPS, __uint_as_float(s), span);
+        if (rest == 0.f) rest = more;
+        s += rest > 0.f ? 1u : rest < 0.f ? ~0u : 0u;
+    }
+    return __bfloat162float(__float2bfloat16_rn(__uint_as_float(s)));
+}
+// The same for hi - lo, hi >= 0 >= lo.
+__device__ __forceinline__ float w4_scale_between(float lo, float hi)
+{
+    const float span = hi - lo, b = span - hi;
+    return w4_scale<15>(span, (hi - (span - b)) - (lo + b));
+}
+
 // grid (KT, NT, E): one tile.  A lane takes the sixteen inputs of two stored words, eight lanes an output row; a
 // group is 2, 4 or 8 neighbouring lanes.  A thread asks for two rows' pieces before it uses the
 // first.  WHOLE: rows of w start at 16-byte boundaries.
@@ -296,7 +317,7 @@ __global__ void __launch_bounds__(256) bls_w4_quantize_kernel(const void *wv, lo
                 if (ZERO) lo = fminf(lo, __shfl_xor_sync(~0u, lo, o));
                 hi = fmaxf(hi, __shfl_xor_sync(~0u, hi, o));
             }
-            float s = __bfloat162float(__float2bfloat16_rn(ZERO ? __fdiv_rn(hi - lo, 15.f) : __fdiv_rn(hi, 7.f)));
+            float s = ZERO ? w4_scale_between(lo, hi) : w4_scale<7>(hi, 0.f);
             if (!isfinite(s)) s = __int_as_float(0x7fc00000);                // the whole group becomes NaN
             const __nv_bfloat16 sb = __float2bfloat16_rn(s);
             const bool usable = s > 0.f;
