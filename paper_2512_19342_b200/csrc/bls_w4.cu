@@ -256,11 +256,13 @@ __device__ __forceinline__ float w4_scale(float span, float more)
     }
     return __bfloat162float(__float2bfloat16_rn(__uint_as_float(s)));
 }
-// The same for hi - lo, hi >= 0 >= lo.
+// The same for hi - lo, hi >= 0 >= lo.  A difference past fp32's range is taken in halves.
 __device__ __forceinline__ float w4_scale_between(float lo, float hi)
 {
+    const float part = isinf(hi - lo) ? 0.5f : 1.f;
+    hi *= part; lo *= part;
     const float span = hi - lo, b = span - hi;
-    return w4_scale<15>(span, (hi - (span - b)) - (lo + b));
+    return w4_scale<15>(span, (hi - (span - b)) - (lo + b)) / part;
 }
 
 // grid (KT, NT, E): one tile.  A lane takes the sixteen inputs of two stored words, eight lanes an output row; a

@@ -83,6 +83,22 @@ def test_scales_of_tiny_weights():
     assert np.array_equal(got, want)
 
 
+def test_scales_of_spans_past_the_range():
+    """hi - lo passes fp32's range, the scale does not: the group is held, each weight to within half a step and half a zero point's step."""
+    big = float(np.ldexp(255.0, 120))
+    rows = [(big, -big), (big, -big / 2, big / 3, -big / 5, 1.0), (big / 4, -big), (big * 0.75, -big * 0.75, 0.25 * big)]
+    w = group_of([[float(np.float32(v)) for v in r] for r in rows])
+    got, want = scales(w, False)
+    assert np.array_equal(got, want)
+    t = bls.bls_w4_quantize(w, GROUP, False)
+    q = torch.empty_like(w)
+    bls.bls_w4_dequantize(t, q)
+    fine = torch.isfinite(q)
+    assert bool((fine | (w.abs() >= 0.9 * big)).all())       # (q - z) s of the largest weight may itself pass the range
+    off = (q.double() - w.double()).abs()
+    assert bool((off <= 1.25 * torch.from_numpy(want).cuda())[fine].all())
+
+
 def plain_forms():
     spec = importlib.util.spec_from_file_location("operators_cases", os.path.join(ROOT, "perf", "operators.py"))
     m = importlib.util.module_from_spec(spec)
