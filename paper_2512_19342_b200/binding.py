@@ -585,21 +585,46 @@ def bls_moe_combine_grad(dout: torch.Tensor, y: Optional[torch.Tensor], place: t
 
 
 class W4:
-    """E matrices [N][K] in 4 bits with group scales: the three tensors of the storage format (include/bls.h)."""
-    __slots__ = ("q", "scale", "zero", "E", "N", "K", "group", "_args")
+    """E matrices [N][K] in 4 bits with group scales: the three tensors of the storage format (include/bls.h).  The tensors and sizes are
+    set once, so that they fit each other; other weights are another W4.  Their contents may be written, and their memory may move
+    (q.data = ...): every call looks at where they are, and checks them again after a move."""
+    __slots__ = ("_tensors", "_sizes", "_at")
 
     def __init__(self, q: torch.Tensor, scale: torch.Tensor, zero: Optional[torch.Tensor], N: int, K: int, group: int):
         if group not in (32, 64, 128) or N < 1 or K < 1 or q.dim() != 5:
             raise ValueError("W4: bad sizes")
-        nt, kt, E = (N + 127) // 128, (K + 127) // 128, q.shape[0]
-        shape = (E, kt * 128 // group, nt * 128)
-        self._set(_flat(q, "q", (E, nt, kt, 128, 64), torch.uint8), _flat(scale, "scale", shape, torch.bfloat16),
-                  _flat(zero, "zero", shape, torch.uint8), q, scale, zero, E, N, K, group)
+        self._tensors, self._sizes = (q, scale, zero), (q.shape[0], N, K, group)
+        self._check()
 
-    def _set(self, pq, ps, pz, q, scale, zero, E, N, K, group):
-        self._args = (pq, ps, pz, E, N, K, group)
-        self.q, self.scale, self.zero, self.E, self.N, self.K, self.group = q, scale, zero, E, N, K, group
-        return self
+    @classmethod
+    def _of(cls, tensors, sizes, at) -> "W4":
+        """A W4 of tensors that are known to fit."""
+        w4 = cls.__new__(cls)
+        w4._tensors, w4._sizes, w4._at = tensors, sizes, at
+        return w4
+
+    def _check(self):
+        (q, scale, zero), (E, N, K, group) = self._tensors, self._sizes
+        nt, kt = (N + 127) // 128, (K + 127) // 128
+        shape = (E, kt * 128 // group, nt * 128)
+        self._at = (_flat(q, "q", (E, nt, kt, 128, 64), torch.uint8), _flat(scale, "scale", shape, torch.bfloat16),
+                    _flat(zero, "zero", shape, torch.uint8))
+
+    @property
+    def _args(self) -> tuple:
+        """The addresses of q, scale and zero, as they are now, and the sizes."""
+        q, scale, zero = self._tensors
+        if (q.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr()) != self._at:
+            self._check()
+        return self._at + self._sizes
+
+    q = property(lambda self: self._tensors[0])
+    scale = property(lambda self: self._tensors[1])
+    zero = property(lambda self: self._tensors[2])
+    E = property(lambda self: self._sizes[0])
+    N = property(lambda self: self._sizes[1])
+    K = property(lambda self: self._sizes[2])
+    group = property(lambda self: self._sizes[3])
 
 
 def bls_w4_sizes(E: int, N: int, K: int, group: int):
@@ -635,14 +660,14 @@ def bls_w4_quantize(w: torch.Tensor, group: int = 128, symmetric: bool = True, s
     code = lib().bls_w4_quantize(w.data_ptr(), _DTYPE[w.dtype], ld, E, N, K, group, pq, ps, pz, _on(stream, w))
     if code:
         raise BlsError(code, "bls_w4_quantize")
-    return W4.__new__(W4)._set(pq, ps, pz, q, scale, zero, E, N, K, group)
+    return W4._of((q, scale, zero), (E, N, K, group), (pq, ps, pz))
 
 
 def bls_w4_dequantize(w4: W4, w: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """w [E][N][K] (or [N][K] with E = 1) = (q - z) * s, rounded once to w's type."""
     E, N, K, ld = _matrices(w, "w")
-    if (E, N, K) != (w4.E, w4.N, w4.K):
-        raise ValueError(f"w: expected {(w4.E, w4.N, w4.K)}")
+    if (E, N, K) != w4._sizes[:3]:
+        raise ValueError(f"w: expected {w4._sizes[:3]}")
     code = lib().bls_w4_dequantize(*w4._args, w.data_ptr(), _DTYPE[w.dtype], ld, _on(stream, w))
     if code:
         raise BlsError(code, "bls_w4_dequantize")
@@ -673,7 +698,7 @@ def bls_w4_linear(w4: W4, x: torch.Tensor, y: torch.Tensor, offsets: Optional[to
     """y = act(x W^T + bias), row by row with the matrix that offsets int32 [E+1] gives it (None with E = 1); rows from
     offsets[-1] on become 0.  x [rows][K] bf16 or f16, y [rows][N] bf16, f16 or fp32, bias fp32 [E][N];
     act 0 none, 1 ReLU, 2 logistic function.  The first call on a device sets up its status word and synchronises: make it before any capture."""
-    E, N, K = w4.E, w4.N, w4.K
+    E, N, K, _ = w4._sizes
     rows = _two(x, "x")[0]
     if x.dtype is _F32 or (offsets is None and E != 1):
         raise ValueError("x: expected bf16 or f16" if x.dtype is _F32 else "offsets are needed with more than one matrix")
