@@ -462,11 +462,34 @@ def bls_interact(x: torch.Tensor, pooled: torch.Tensor, r: torch.Tensor, stream:
 
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
     lambda device: torch.cuda.current_stream(device).cuda_stream
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
 
-def _on(stream: Optional[torch.cuda.Stream], like: torch.Tensor) -> int:
-    """Handle of the stream that a call on `like` is enqueued on."""
-    return _raw_stream(like.get_device()) if stream is None else stream.cuda_stream
+def _gpu(t: torch.Tensor, name: str, stream: Optional[torch.cuda.Stream]) -> int:
+    """The device of a call: that of its first tensor.  All other tensors and the stream have to be there too."""
+    device = t.get_device()
+    if device < 0:
+        raise ValueError(f"{name}: expected a CUDA tensor, got one on {t.device}")
+    if stream is not None and stream.device_index != device:
+        raise ValueError(f"stream: expected one of cuda:{device}, where {name} is, got one of cuda:{stream.device_index}")
+    return device
+
+
+def _on(stream: Optional[torch.cuda.Stream], device: int) -> int:
+    """Handle of the stream that a call is enqueued on."""
+    return _raw_stream(device) if stream is None else stream.cuda_stream
+
+
+def _enqueue(name: str, device: int, *args):
+    """One call of the library with the tensors' device as the current one."""
+    call = getattr(lib(), name)
+    if _current_device() == device:
+        code = call(*args)
+    else:
+        with torch.cuda.device(device):
+            code = call(*args)
+    if code:
+        raise BlsError(code, name)
 
 
 def _scratch(n: int, stream: Optional[torch.cuda.Stream], like: torch.Tensor) -> torch.Tensor:
@@ -482,24 +505,24 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
-def _flat(t: Optional[torch.Tensor], name: str, shape: tuple, dtype: torch.dtype):
-    """Address of a contiguous tensor of one shape and type on a GPU (None stays None)."""
+def _flat(t: Optional[torch.Tensor], name: str, shape: tuple, dtype: torch.dtype, device: int):
+    """Address of a contiguous tensor of one shape and type on one GPU (None stays None)."""
     if t is None:
         return None
-    if t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+    if t.get_device() == device and t.dtype is dtype and t.shape == shape and t.is_contiguous():
         return t.data_ptr()
-    raise ValueError(f"{name}: expected a contiguous CUDA tensor {shape} of {dtype}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    raise ValueError(f"{name}: expected a contiguous tensor {shape} of {dtype} on cuda:{device}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
 
 
-def _rows(t: torch.Tensor, name: str, shape: tuple, dtype: torch.dtype):
-    """(address, row pitch) of a matrix of one type on a GPU whose rows are contiguous, at any pitch."""
-    if t.is_cuda and t.dtype is dtype and t.shape == shape:
+def _rows(t: torch.Tensor, name: str, shape: tuple, dtype: torch.dtype, device: int):
+    """(address, row pitch) of a matrix of one type on one GPU whose rows are contiguous, at any pitch."""
+    if t.get_device() == device and t.dtype is dtype and t.shape == shape:
         ld, step = t.stride()
         if step == 1 and ld >= shape[1] > 0:
             return t.data_ptr(), ld
         if (step == 1 or shape[1] < 2) and (ld >= shape[1] or shape[0] < 2):     # one row or column: its strides say nothing
             return t.data_ptr(), max(ld, shape[1], 1)
-    raise ValueError(f"{name}: expected a CUDA matrix {shape} of {dtype} with contiguous rows, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}, on {t.device}")
+    raise ValueError(f"{name}: expected a matrix {shape} of {dtype} with contiguous rows on cuda:{device}, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}, on {t.device}")
 
 
 def _two(t: torch.Tensor, name: str) -> tuple:
@@ -523,18 +546,16 @@ def bls_moe_route(expert: torch.Tensor, n_experts: int, order: torch.Tensor, pla
     """Stable sort of the slots expert int32 [n][k] by expert; IDs outside [0, n_experts) leave their slot out.
     order int32 [n*k], place int32 [n][k], offsets int32 [n_experts+1] are written."""
     n, k = _two(expert, "expert")
-    args = (_flat(expert, "expert", (n, k), _I32), n, k, n_experts, _flat(order, "order", (n * k,), _I32),
-            _flat(place, "place", (n, k), _I32), _flat(offsets, "offsets", (n_experts + 1,), _I32))
-    l = lib()
+    dev = _gpu(expert, "expert", stream)
+    args = (_flat(expert, "expert", (n, k), _I32, dev), n, k, n_experts, _flat(order, "order", (n * k,), _I32, dev),
+            _flat(place, "place", (n, k), _I32, dev), _flat(offsets, "offsets", (n_experts + 1,), _I32, dev))
     ws, nbytes = None, 0
     if n * k > 4096:                         # fewer slots never need a workspace
         size = C.c_size_t(0)
-        _check(l.bls_moe_bytes(n, k, n_experts, C.byref(size)), "bls_moe_bytes")
+        _check(lib().bls_moe_bytes(n, k, n_experts, C.byref(size)), "bls_moe_bytes")
         nbytes = size.value
         ws = _scratch(nbytes, stream, expert)
-    code = l.bls_moe_route(*args, ws.data_ptr() if nbytes else None, nbytes, _on(stream, expert))
-    if code:
-        raise BlsError(code, "bls_moe_route")
+    _enqueue("bls_moe_route", dev, *args, ws.data_ptr() if nbytes else None, nbytes, _on(stream, dev))
 
 
 def bls_moe_dispatch(x: torch.Tensor, place: torch.Tensor, offsets: torch.Tensor, y: torch.Tensor,
@@ -542,13 +563,12 @@ def bls_moe_dispatch(x: torch.Tensor, place: torch.Tensor, offsets: torch.Tensor
     """y[place[t][i]] = x[t]; the rows of y from offsets[-1] on become 0.  x [n][D], y [rows][D] of one type."""
     n, k = _two(place, "place")
     D, R, dt = _two(x, "x")[1], _two(y, "y")[0], x.dtype
-    px, ldx = _rows(x, "x", (n, D), dt)
-    py, ldy = _rows(y, "y", (R, D), dt)
+    dev = _gpu(x, "x", stream)
+    px, ldx = _rows(x, "x", (n, D), dt, dev)
+    py, ldy = _rows(y, "y", (R, D), dt, dev)
     e = offsets.numel()
-    code = lib().bls_moe_dispatch(px, ldx, _dt(x, "x"), _flat(place, "place", (n, k), _I32), _flat(offsets, "offsets", (e,), _I32), e - 1,
-                                  n, k, D, py, ldy, R, _on(stream, x))
-    if code:
-        raise BlsError(code, "bls_moe_dispatch")
+    _enqueue("bls_moe_dispatch", dev, px, ldx, _dt(x, "x"), _flat(place, "place", (n, k), _I32, dev),
+             _flat(offsets, "offsets", (e,), _I32, dev), e - 1, n, k, D, py, ldy, R, _on(stream, dev))
 
 
 def bls_moe_combine(y: torch.Tensor, place: torch.Tensor, w: Optional[torch.Tensor], out: torch.Tensor,
@@ -556,12 +576,11 @@ def bls_moe_combine(y: torch.Tensor, place: torch.Tensor, w: Optional[torch.Tens
     """out[t] = sum over i of w[t][i] * y[place[t][i]] (w fp32 [n][k] or None: all 1).  y [rows][D], out [n][D] of one type."""
     n, k = _two(place, "place")
     D, R, dt = _two(out, "out")[1], _two(y, "y")[0], y.dtype
-    po, ldo = _rows(out, "out", (n, D), dt)
-    py, ldy = _rows(y, "y", (R, D), dt)
-    code = lib().bls_moe_combine(py, ldy, R, _dt(y, "y"), _flat(place, "place", (n, k), _I32), _flat(w, "w", (n, k), _F32),
-                                 n, k, D, po, ldo, _on(stream, y))
-    if code:
-        raise BlsError(code, "bls_moe_combine")
+    dev = _gpu(y, "y", stream)
+    po, ldo = _rows(out, "out", (n, D), dt, dev)
+    py, ldy = _rows(y, "y", (R, D), dt, dev)
+    _enqueue("bls_moe_combine", dev, py, ldy, R, _dt(y, "y"), _flat(place, "place", (n, k), _I32, dev),
+             _flat(w, "w", (n, k), _F32, dev), n, k, D, po, ldo, _on(stream, dev))
 
 
 def bls_moe_combine_grad(dout: torch.Tensor, y: Optional[torch.Tensor], place: torch.Tensor, offsets: torch.Tensor,
@@ -570,25 +589,24 @@ def bls_moe_combine_grad(dout: torch.Tensor, y: Optional[torch.Tensor], place: t
     """Gradients of bls_moe_combine: dy[place[t][i]] = w[t][i] * dout[t] and, if wanted, dw[t][i] = <dout[t], y[place[t][i]]>."""
     n, k = _two(place, "place")
     D, R, dt = _two(dout, "dout")[1], _two(dy, "dy")[0], dout.dtype
-    pd, ldd = _rows(dout, "dout", (n, D), dt)
-    pg, ldg = _rows(dy, "dy", (R, D), dt)
+    dev = _gpu(dout, "dout", stream)
+    pd, ldd = _rows(dout, "dout", (n, D), dt, dev)
+    pg, ldg = _rows(dy, "dy", (R, D), dt, dev)
     py, ldy = None, D
     if dw is not None:
         _need(y is not None, "dw needs y")
-        py, ldy = _rows(y, "y", (R, D), dt)
+        py, ldy = _rows(y, "y", (R, D), dt, dev)
     e = offsets.numel()
-    code = lib().bls_moe_combine_grad(pd, ldd, py, ldy, R, _dt(dout, "dout"), _flat(place, "place", (n, k), _I32),
-                                      _flat(offsets, "offsets", (e,), _I32), e - 1, _flat(w, "w", (n, k), _F32), n, k, D, pg, ldg,
-                                      _flat(dw, "dw", (n, k), _F32), _on(stream, dout))
-    if code:
-        raise BlsError(code, "bls_moe_combine_grad")
+    _enqueue("bls_moe_combine_grad", dev, pd, ldd, py, ldy, R, _dt(dout, "dout"), _flat(place, "place", (n, k), _I32, dev),
+             _flat(offsets, "offsets", (e,), _I32, dev), e - 1, _flat(w, "w", (n, k), _F32, dev), n, k, D, pg, ldg,
+             _flat(dw, "dw", (n, k), _F32, dev), _on(stream, dev))
 
 
 class W4:
     """E matrices [N][K] in 4 bits with group scales: the three tensors of the storage format (include/bls.h).  The tensors and sizes are
     set once, so that they fit each other; other weights are another W4.  Their contents may be written, and their memory may move
     (q.data = ...): every call looks at where they are, and checks them again after a move."""
-    __slots__ = ("_tensors", "_sizes", "_at")
+    __slots__ = ("_tensors", "_sizes", "_at", "_device")
 
     def __init__(self, q: torch.Tensor, scale: torch.Tensor, zero: Optional[torch.Tensor], N: int, K: int, group: int):
         if group not in (32, 64, 128) or N < 1 or K < 1 or q.dim() != 5:
@@ -597,18 +615,19 @@ class W4:
         self._check()
 
     @classmethod
-    def _of(cls, tensors, sizes, at) -> "W4":
+    def _of(cls, tensors, sizes, at, device) -> "W4":
         """A W4 of tensors that are known to fit."""
         w4 = cls.__new__(cls)
-        w4._tensors, w4._sizes, w4._at = tensors, sizes, at
+        w4._tensors, w4._sizes, w4._at, w4._device = tensors, sizes, at, device
         return w4
 
     def _check(self):
         (q, scale, zero), (E, N, K, group) = self._tensors, self._sizes
         nt, kt = (N + 127) // 128, (K + 127) // 128
         shape = (E, kt * 128 // group, nt * 128)
-        self._at = (_flat(q, "q", (E, nt, kt, 128, 64), torch.uint8), _flat(scale, "scale", shape, torch.bfloat16),
-                    _flat(zero, "zero", shape, torch.uint8))
+        dev = self._device = _gpu(q, "q", None)
+        self._at = (_flat(q, "q", (E, nt, kt, 128, 64), torch.uint8, dev), _flat(scale, "scale", shape, torch.bfloat16, dev),
+                    _flat(zero, "zero", shape, torch.uint8, dev))
 
     @property
     def _args(self) -> tuple:
@@ -617,6 +636,13 @@ class W4:
         if (q.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr()) != self._at:
             self._check()
         return self._at + self._sizes
+
+    def _args_on(self, device: int) -> tuple:
+        """_args of weights that are on this device."""
+        args = self._args
+        if self._device != device:
+            raise ValueError(f"w4: expected weights on cuda:{device}, got some on cuda:{self._device}")
+        return args
 
     q = property(lambda self: self._tensors[0])
     scale = property(lambda self: self._tensors[1])
@@ -651,16 +677,15 @@ def bls_w4_quantize(w: torch.Tensor, group: int = 128, symmetric: bool = True, s
     """Weights [E][N][K] or [N][K] in 4 bits with one scale (and, unless symmetric, one zero point) per `group` inputs."""
     E, N, K, ld = _matrices(w, "w")
     _need(group in (32, 64, 128), "group: 32, 64 or 128")
+    dev = _gpu(w, "w", stream)
     nt, kt = (N + 127) // 128, (K + 127) // 128
     shape = (E, kt * 128 // group, nt * 128)
     with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():      # memory of the call's own stream
         q, scale = w.new_empty((E, nt, kt, 128, 64), dtype=torch.uint8), w.new_empty(shape, dtype=torch.bfloat16)
         zero = None if symmetric else w.new_empty(shape, dtype=torch.uint8)
     pq, ps, pz = q.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr()
-    code = lib().bls_w4_quantize(w.data_ptr(), _DTYPE[w.dtype], ld, E, N, K, group, pq, ps, pz, _on(stream, w))
-    if code:
-        raise BlsError(code, "bls_w4_quantize")
-    return W4._of((q, scale, zero), (E, N, K, group), (pq, ps, pz))
+    _enqueue("bls_w4_quantize", dev, w.data_ptr(), _DTYPE[w.dtype], ld, E, N, K, group, pq, ps, pz, _on(stream, dev))
+    return W4._of((q, scale, zero), (E, N, K, group), (pq, ps, pz), dev)
 
 
 def bls_w4_dequantize(w4: W4, w: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
@@ -668,9 +693,8 @@ def bls_w4_dequantize(w4: W4, w: torch.Tensor, stream: Optional[torch.cuda.Strea
     E, N, K, ld = _matrices(w, "w")
     if (E, N, K) != w4._sizes[:3]:
         raise ValueError(f"w: expected {w4._sizes[:3]}")
-    code = lib().bls_w4_dequantize(*w4._args, w.data_ptr(), _DTYPE[w.dtype], ld, _on(stream, w))
-    if code:
-        raise BlsError(code, "bls_w4_dequantize")
+    dev = _gpu(w, "w", stream)
+    _enqueue("bls_w4_dequantize", dev, *w4._args_on(dev), w.data_ptr(), _DTYPE[w.dtype], ld, _on(stream, dev))
 
 
 _w4_status_word = {}                         # device number -> (int32 [1], its address), zeroed once: waits that gave up are latched here
@@ -702,17 +726,16 @@ def bls_w4_linear(w4: W4, x: torch.Tensor, y: torch.Tensor, offsets: Optional[to
     rows = _two(x, "x")[0]
     if x.dtype is _F32 or (offsets is None and E != 1):
         raise ValueError("x: expected bf16 or f16" if x.dtype is _F32 else "offsets are needed with more than one matrix")
-    px, ldx = _rows(x, "x", (rows, K), x.dtype)
-    py, ldy = _rows(y, "y", (rows, N), y.dtype)
-    l = lib()
+    dev = _gpu(x, "x", stream)
+    px, ldx = _rows(x, "x", (rows, K), x.dtype, dev)
+    py, ldy = _rows(y, "y", (rows, N), y.dtype, dev)
     ws, nbytes = None, 0
     if rows > 8:                             # fewer rows never need a workspace
         size = C.c_size_t(0)
-        _check(l.bls_w4_bytes(E, N, K, px, ldx, rows, C.byref(size)), "bls_w4_bytes")
+        _check(lib().bls_w4_bytes(E, N, K, px, ldx, rows, C.byref(size)), "bls_w4_bytes")
         nbytes = size.value
         if nbytes:
             ws = _scratch(nbytes, stream, x)
-    code = l.bls_w4_linear(*w4._args, px, _dt(x, "x"), ldx, rows, _flat(offsets, "offsets", (E + 1,), _I32), _flat(bias, "bias", (E, N), _F32),
-                           act, py, _dt(y, "y"), ldy, ws.data_ptr() if nbytes else None, nbytes, _status_word(x.get_device())[1], _on(stream, x))
-    if code:
-        raise BlsError(code, "bls_w4_linear")
+    _enqueue("bls_w4_linear", dev, *w4._args_on(dev), px, _dt(x, "x"), ldx, rows, _flat(offsets, "offsets", (E + 1,), _I32, dev),
+             _flat(bias, "bias", (E, N), _F32, dev), act, py, _dt(y, "y"), ldy, ws.data_ptr() if nbytes else None, nbytes,
+             _status_word(dev)[1], _on(stream, dev))
