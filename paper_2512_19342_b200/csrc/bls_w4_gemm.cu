@@ -16,8 +16,9 @@
 //
 // Roles: warps 0-3 unpack, warps 4-11 scale and store, one thread of warp 12 loads (TMA for x, bulk
 // copies for the weight tile and its scales and zero points), one thread of warp 13 issues the
-// products.  Every wait is bounded by the clock: one that gives up latches BLS_ST_ETIMEOUT, all
-// roles wind down and tensor memory is released.
+// products.  Every wait on an mbarrier is bounded by the clock: one that gives up latches BLS_ST_ETIMEOUT, all
+// roles wind down and tensor memory is released.  The cluster barriers of the split form have no limit of their
+// own: every role of every CTA arrives at both, at the end of its loop or after a wait that gave up.
 #include "bls_tc.cuh"
 #include "bls_w4.cuh"
 #include "bls_w4_gemm.h"
@@ -134,8 +135,10 @@ __device__ __forceinline__ void gm_store_rows(Y *at, long long ldy, int rows, in
     }
 }
 
+// The .aligned barrier wants whole warps, and callers come out of code that goes lane by lane.
 __device__ __forceinline__ void cluster_sync()
 {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
@@ -487,7 +490,6 @@ __global__ void __launch_bounds__(GM_THREADS, 1) bls_w4_tiles_kernel(const __gri
         }
     }
     if (SPLIT && (warp < 4 || warp >= 12)) {
-        __syncwarp();
         cluster_sync();
         cluster_sync();
     }
