@@ -106,7 +106,7 @@ bls_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         // epilogue: warp w reads TMEM lanes 32 (w mod 4) .. +31, one row of the tile per thread
         const int q = warp & 3;
         const int row = m0 + q * 32 + lane;
-        if (mb_wait(done_bar, 0, a.status)) {
+        if (__all_sync(~0u, mb_wait(done_bar, 0, a.status))) {                // one verdict: tcgen05.ld wants the whole warp
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             // bf16 output with whole 16-byte pieces: the warp's 32 x BN block goes through shared memory (the
             // tile ring is free: every MMA that read it has completed) and leaves as coalesced row pieces
