@@ -10,6 +10,7 @@ import collections
 import contextlib
 import ctypes as C
 import os
+import threading
 from typing import Optional, Sequence
 
 import torch
@@ -698,14 +699,18 @@ def bls_w4_dequantize(w4: W4, w: torch.Tensor, stream: Optional[torch.cuda.Strea
 
 
 _w4_status_word = {}                         # device number -> (int32 [1], its address), zeroed once: waits that gave up are latched here
+_w4_status_lock = threading.Lock()           # one word for each device, whichever thread asks first
 
 
 def _status_word(device: int):
     t = _w4_status_word.get(device)
     if t is None:
-        word = torch.zeros(1, dtype=_I32, device=torch.device("cuda", device))
-        torch.cuda.synchronize(device)       # once: calls on any stream may use it from here on
-        t = _w4_status_word[device] = (word, word.data_ptr())
+        with _w4_status_lock:
+            t = _w4_status_word.get(device)
+            if t is None:
+                word = torch.zeros(1, dtype=_I32, device=torch.device("cuda", device))
+                torch.cuda.synchronize(device)       # once: calls on any stream may use it from here on
+                t = _w4_status_word[device] = (word, word.data_ptr())
     return t
 
 

@@ -1,5 +1,8 @@
 """What the expert stage's Python calls check and keep, without a GPU: stand-in tensors that only have an address, and a
 stand-in library that notes its calls.  Nothing is launched."""
+import threading
+import time
+
 import pytest
 import torch
 
@@ -160,3 +163,29 @@ def test_calls_run_on_their_tensors_gpu(notes, device, current):
             call(tensors, stream)
             (called, args, at), = notes.calls
             assert called == name and args[-1] == handle and at == device and notes.current == current
+
+
+def test_one_status_word_however_many_threads_ask(monkeypatch):
+    """A launch holds the word's address, so a second word must never replace the first."""
+    made = []
+
+    def zeros(*_, **__):
+        made.append(threading.current_thread())
+        time.sleep(0.05)                                      # the others arrive meanwhile
+        return Stub((1,), I32, 0, (1 << 20) + 256 * len(made))
+
+    monkeypatch.setattr(binding, "_w4_status_word", {})
+    monkeypatch.setattr(torch, "zeros", zeros)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda *_: None)
+    start, got = threading.Barrier(8), []
+
+    def ask():
+        start.wait()
+        got.append(binding._status_word(0))
+
+    threads = [threading.Thread(target=ask) for _ in range(8)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(made) == 1 and len(got) == 8 and all(w is got[0] for w in got)
