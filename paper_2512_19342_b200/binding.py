@@ -715,11 +715,16 @@ def _status_word(device: int):
 
 
 def bls_w4_status(device=None) -> int:
-    """Synchronises the device; BLS_ETIMEOUT if a bounded wait inside a 4-bit product gave up."""
+    """Synchronises the device; BLS_ETIMEOUT if a bounded wait inside a 4-bit product gave up since the last call."""
     index = torch.device("cuda" if device is None else device).index
     index = torch.cuda.current_device() if index is None else index
     torch.cuda.synchronize(index)
-    return BLS_ETIMEOUT if int(_status_word(index)[0].item()) & 8 else BLS_OK
+    word = _status_word(index)[0]
+    if not int(word.item()) & 8:
+        return BLS_OK
+    word.zero_()
+    torch.cuda.synchronize(index)
+    return BLS_ETIMEOUT
 
 
 def bls_w4_linear(w4: W4, x: torch.Tensor, y: torch.Tensor, offsets: Optional[torch.Tensor] = None,

@@ -189,3 +189,14 @@ def test_one_status_word_however_many_threads_ask(monkeypatch):
     for t in threads:
         t.join()
     assert len(made) == 1 and len(got) == 8 and all(w is got[0] for w in got)
+
+
+def test_a_time_out_is_reported_once(monkeypatch):
+    word = torch.zeros(1, dtype=torch.int32)
+    monkeypatch.setattr(binding, "_w4_status_word", {0: (word, 7)})
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda *_: None)
+    assert bls.bls_w4_status("cuda:0") == bls.BLS_OK
+    for _ in range(2):
+        word.fill_(8)                                         # what a wait that gives up leaves there
+        assert bls.bls_w4_status("cuda:0") == bls.BLS_ETIMEOUT
+        assert bls.bls_w4_status("cuda:0") == bls.BLS_OK
