@@ -30,6 +30,13 @@ class Routes:
         bls.bls_moe_route(expert, n_experts, self.order, self.place, self.offsets)
 
 
+def _first_derivative_only():
+    """The kernels' results are constants to autograd: where a graph of the gradients is asked for, terms would be missing from it.
+    (once_differentiable does not see this where only saved tensors need gradients.)"""
+    if torch.is_grad_enabled():
+        raise RuntimeError("dispatch and combine have first derivatives only: no create_graph")
+
+
 class _Dispatch(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, routes):
@@ -40,6 +47,7 @@ class _Dispatch(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
+        _first_derivative_only()
         dx = dy.new_empty(ctx.routes.place.shape[0], dy.shape[1])
         bls.bls_moe_combine(dy.contiguous(), ctx.routes.place, None, dx)
         return dx, None
@@ -56,6 +64,7 @@ class _Combine(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dout):
+        _first_derivative_only()
         y, w = ctx.saved_tensors
         dy, dw = torch.empty_like(y), torch.empty_like(w)
         bls.bls_moe_combine_grad(dout.contiguous(), y, ctx.routes.place, ctx.routes.offsets, w, dy, dw)
@@ -63,12 +72,12 @@ class _Combine(torch.autograd.Function):
 
 
 def dispatch(x: torch.Tensor, routes: Routes) -> torch.Tensor:
-    """Rows of x [n][D] at their sorted places [n * k][D]; differentiable in x."""
+    """Rows of x [n][D] at their sorted places [n * k][D]; differentiable once in x."""
     return _Dispatch.apply(x, routes)
 
 
 def combine(y: torch.Tensor, w: torch.Tensor, routes: Routes) -> torch.Tensor:
-    """Weighted sums [n][D] of the sorted rows y [n * k][D], w fp32 [n][k]; differentiable in y and w."""
+    """Weighted sums [n][D] of the sorted rows y [n * k][D], w fp32 [n][k]; differentiable once in y and w."""
     return _Combine.apply(y, w, routes)
 
 

@@ -1,8 +1,14 @@
 """How the expert stage's calls treat their memory, streams and threads, beside what they compute.  GPU only."""
+import os
+import sys
+
 import pytest
 import torch
 
-import paper_2512_19342_b200 as bls
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+
+import expert_stage as ex  # noqa: E402
+import paper_2512_19342_b200 as bls  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +40,23 @@ def test_weights_whose_memory_moves(rows):
         bls.bls_w4_linear(t, x, y1)
     with pytest.raises(ValueError):
         bls.bls_w4_dequantize(t, w1)
+
+
+def test_second_derivatives_are_refused():
+    """d out / d x depends on w: a graph of the gradient that leaves this out must not come back."""
+    n, k, E, D = 20, 2, 4, 24
+    g = gen(5)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g)
+    routes = ex.Routes(torch.randint(0, E, (n, k), device="cuda", generator=g, dtype=torch.int32), E)
+    x, w = rnd(n, D).requires_grad_(), rnd(n, k).requires_grad_()
+    out = ex.combine(ex.dispatch(x, routes), w, routes).sum()
+    with pytest.raises(RuntimeError, match="first derivatives"):
+        torch.autograd.grad(out, (x, w), create_graph=True)
+    only = ex.dispatch(x, routes).sum()
+    with pytest.raises(RuntimeError, match="first derivatives"):
+        torch.autograd.grad(only, x, create_graph=True)
+    again = ex.combine(ex.dispatch(x, routes), w, routes).sum()
+    dx, dw = torch.autograd.grad(again, (x, w))
+    # fp32 sums: k terms for dx, D products for dw, two more roundings each
+    assert bool(((dx - w.sum(1, keepdim=True)).abs() <= 2 * (k + 2) * 2.0 ** -24 * w.abs().sum(1, keepdim=True)).all())
+    assert bool(((dw - x.sum(1, keepdim=True)).abs() <= 2 * (D + 2) * 2.0 ** -24 * x.abs().sum(1, keepdim=True)).all())
