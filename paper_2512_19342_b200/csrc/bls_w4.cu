@@ -324,8 +324,8 @@ __global__ void __launch_bounds__(256) bls_w4_quantize_kernel(const void *wv, lo
             const __nv_bfloat16 sb = __float2bfloat16_rn(s);
             const bool usable = s > 0.f;
             const int z = !ZERO || nt * W4_TILE + r >= d.N ? 8 : usable ? (int)fminf(fmaxf(rintf(__fdiv_rn(-lo, s)), 0.f), 15.f) : 0;
-            // above 1e37 the reciprocal would be subnormal and lose bits
-            const float inv = usable && s < 1e37f ? __fdividef(1.f, s) : __int_as_float(0x7fc00000);
+            // above 1e37 the reciprocal would be subnormal and lose bits, below 2^-126 the fast division is not defined
+            const float inv = s >= 0x1p-126f && s < 1e37f ? __fdividef(1.f, s) : __int_as_float(0x7fc00000);
             const float below = inv * (1.f - 0x1p-19f), above = inv * (1.f + 0x1p-19f);
             constexpr float ROUND = 12582912.f;                              // 1.5 2^23
             constexpr unsigned BITS = 0x4b400000u;                           // its bits

@@ -83,6 +83,23 @@ def test_scales_of_tiny_weights():
     assert np.array_equal(got, want)
 
 
+@pytest.mark.parametrize("symmetric", [True, False], ids=["symmetric", "zeros"])
+def test_weights_of_every_magnitude(symmetric):
+    """Groups from the smallest to the largest numbers, around the end of the normal range above all: the stored weights are those of the
+    fp32 quotients by the scale, which numpy divides the same way."""
+    g = np.random.default_rng(6)
+    size = np.concatenate([np.exp2(g.uniform(-149, 126, 3000)), np.exp2(g.uniform(-130, -120, 3000))])
+    w = (g.uniform(-1, 1, (size.size, GROUP)) * size[:, None]).astype(np.float32)
+    t = bls.bls_w4_quantize(torch.from_numpy(w).cuda(), GROUP, symmetric)
+    s = t.scale[0, 0, :size.size].float().cpu().numpy()
+    safe = np.where(s > 0, s, np.float32(1))
+    z = np.full(size.size, 8, np.float32) if symmetric else np.where(s > 0, np.clip(np.rint(np.maximum(-w.min(1), 0) / safe), 0, 15), 0)
+    q = np.clip(np.where(s[:, None] > 0, np.rint(w / safe[:, None]), 0) + z[:, None], 0, 15)
+    back = torch.empty(size.size, GROUP, device="cuda")
+    bls.bls_w4_dequantize(t, back)
+    assert np.array_equal(back.cpu().numpy(), (q - z[:, None]).astype(np.float32) * s[:, None])
+
+
 def test_scales_of_spans_past_the_range():
     """hi - lo passes fp32's range, the scale does not: the group is held, each weight to within half a step and half a zero point's step."""
     big = float(np.ldexp(255.0, 120))
