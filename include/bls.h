@@ -421,16 +421,16 @@ bls_status_t bls_moe_combine_grad(const void *dout, int64_t ldd, const void *y, 
  *                      makes its whole group NaN.  s is the exact quotient rounded once; the quotients by s are fp32.
  *   bls_w4_dequantize  the weights (q - z) * s in fp32, rounded once to dtype
  *   bls_w4_bytes       workspace of bls_w4_linear for these x, ldx and rows (256-byte aligned; 0 up to
- *                      8 rows, and when rows of x start at 16-byte boundaries)
+ *                      8 E rows, and when rows of x start at 16-byte boundaries)
  *   bls_w4_linear      y[r][n] = act(bias[e][n] + sum over groups of s * sum of (q - z) * x[r][..]), e = the
  *                      matrix of row r: rows offsets[e] .. offsets[e + 1] - 1 (int32 [E + 1], as bls_moe_route
- *                      gives them; NULL with E = 1: all rows).  Rows from offsets[E] on are set to 0.
+ *                      gives them, from 0 on; NULL with E = 1: all rows).  Rows from offsets[E] on are set to 0.
  *                      x BLS_BF16 or BLS_F16 [rows][ldx], y [rows][ldy] of y_dtype (any of the three); bias fp32
  *                      [E][N] or NULL; act 0 none, 1 ReLU, 2 logistic function.  q - z is exact in
  *                      x's type, products are summed in fp32 group by group and scaled in fp32: weights
  *                      are never rounded.  rows may be 0.
  *                      status: one int32 of device memory, zeroed by the caller before the first call; a
- *                      bounded wait that gives up sets bit 8 in it (BLS_ETIMEOUT) and y is then incomplete */
+ *                      bounded wait that gives up sets the bit of value 8 in it (BLS_ETIMEOUT) and y is then incomplete */
 bls_status_t bls_w4_sizes(int E, int N, int K, int group, int64_t *q_bytes /*host*/, int64_t *scale_elems /*host*/);
 bls_status_t bls_w4_quantize(const void *w, int dtype, int64_t ldw, int E, int N, int K, int group, uint8_t *q, void *scale,
                              uint8_t *zero, void *cuda_stream);

@@ -481,16 +481,15 @@ def _on(stream: Optional[torch.cuda.Stream], device: int) -> int:
     return _raw_stream(device) if stream is None else stream.cuda_stream
 
 
-def _enqueue(name: str, device: int, *args):
+def _enqueue(call, device: int, *args):
     """One call of the library with the tensors' device as the current one."""
-    call = getattr(lib(), name)
     if _current_device() == device:
         code = call(*args)
     else:
         with torch.cuda.device(device):
             code = call(*args)
     if code:
-        raise BlsError(code, name)
+        raise BlsError(code, call.__name__)
 
 
 def _scratch(n: int, stream: Optional[torch.cuda.Stream], like: torch.Tensor) -> torch.Tensor:
@@ -556,7 +555,7 @@ def bls_moe_route(expert: torch.Tensor, n_experts: int, order: torch.Tensor, pla
         _check(lib().bls_moe_bytes(n, k, n_experts, C.byref(size)), "bls_moe_bytes")
         nbytes = size.value
         ws = _scratch(nbytes, stream, expert)
-    _enqueue("bls_moe_route", dev, *args, ws.data_ptr() if nbytes else None, nbytes, _on(stream, dev))
+    _enqueue(lib().bls_moe_route, dev, *args, ws.data_ptr() if nbytes else None, nbytes, _on(stream, dev))
 
 
 def bls_moe_dispatch(x: torch.Tensor, place: torch.Tensor, offsets: torch.Tensor, y: torch.Tensor,
@@ -568,7 +567,7 @@ def bls_moe_dispatch(x: torch.Tensor, place: torch.Tensor, offsets: torch.Tensor
     px, ldx = _rows(x, "x", (n, D), dt, dev)
     py, ldy = _rows(y, "y", (R, D), dt, dev)
     e = offsets.numel()
-    _enqueue("bls_moe_dispatch", dev, px, ldx, _dt(x, "x"), _flat(place, "place", (n, k), _I32, dev),
+    _enqueue(lib().bls_moe_dispatch, dev, px, ldx, _dt(x, "x"), _flat(place, "place", (n, k), _I32, dev),
              _flat(offsets, "offsets", (e,), _I32, dev), e - 1, n, k, D, py, ldy, R, _on(stream, dev))
 
 
@@ -580,7 +579,7 @@ def bls_moe_combine(y: torch.Tensor, place: torch.Tensor, w: Optional[torch.Tens
     dev = _gpu(y, "y", stream)
     po, ldo = _rows(out, "out", (n, D), dt, dev)
     py, ldy = _rows(y, "y", (R, D), dt, dev)
-    _enqueue("bls_moe_combine", dev, py, ldy, R, _dt(y, "y"), _flat(place, "place", (n, k), _I32, dev),
+    _enqueue(lib().bls_moe_combine, dev, py, ldy, R, _dt(y, "y"), _flat(place, "place", (n, k), _I32, dev),
              _flat(w, "w", (n, k), _F32, dev), n, k, D, po, ldo, _on(stream, dev))
 
 
@@ -598,9 +597,15 @@ def bls_moe_combine_grad(dout: torch.Tensor, y: Optional[torch.Tensor], place: t
         _need(y is not None, "dw needs y")
         py, ldy = _rows(y, "y", (R, D), dt, dev)
     e = offsets.numel()
-    _enqueue("bls_moe_combine_grad", dev, pd, ldd, py, ldy, R, _dt(dout, "dout"), _flat(place, "place", (n, k), _I32, dev),
+    _enqueue(lib().bls_moe_combine_grad, dev, pd, ldd, py, ldy, R, _dt(dout, "dout"), _flat(place, "place", (n, k), _I32, dev),
              _flat(offsets, "offsets", (e,), _I32, dev), e - 1, _flat(w, "w", (n, k), _F32, dev), n, k, D, pg, ldg,
              _flat(dw, "dw", (n, k), _F32, dev), _on(stream, dev))
+
+
+def _w4_shapes(E: int, N: int, K: int, group: int):
+    """Shapes of q and of scale (and zero) of the storage format."""
+    nt, kt = (N + 127) // 128, (K + 127) // 128
+    return (E, nt, kt, 128, 64), (E, kt * 128 // group, nt * 128)
 
 
 class W4:
@@ -623,20 +628,20 @@ class W4:
         return w4
 
     def _check(self):
-        (q, scale, zero), (E, N, K, group) = self._tensors, self._sizes
-        nt, kt = (N + 127) // 128, (K + 127) // 128
-        shape = (E, kt * 128 // group, nt * 128)
+        (q, scale, zero), (stored, shape) = self._tensors, _w4_shapes(*self._sizes)
         dev = self._device = _gpu(q, "q", None)
-        self._at = (_flat(q, "q", (E, nt, kt, 128, 64), torch.uint8, dev), _flat(scale, "scale", shape, torch.bfloat16, dev),
+        self._at = (_flat(q, "q", stored, torch.uint8, dev), _flat(scale, "scale", shape, torch.bfloat16, dev),
                     _flat(zero, "zero", shape, torch.uint8, dev))
 
     @property
     def _args(self) -> tuple:
         """The addresses of q, scale and zero, as they are now, and the sizes."""
         q, scale, zero = self._tensors
-        if (q.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr()) != self._at:
+        at = self._at
+        if q.data_ptr() != at[0] or scale.data_ptr() != at[1] or (zero is not None and zero.data_ptr() != at[2]):
             self._check()
-        return self._at + self._sizes
+            at = self._at
+        return at + self._sizes
 
     def _args_on(self, device: int) -> tuple:
         """_args of weights that are on this device."""
@@ -679,13 +684,12 @@ def bls_w4_quantize(w: torch.Tensor, group: int = 128, symmetric: bool = True, s
     E, N, K, ld = _matrices(w, "w")
     _need(group in (32, 64, 128), "group: 32, 64 or 128")
     dev = _gpu(w, "w", stream)
-    nt, kt = (N + 127) // 128, (K + 127) // 128
-    shape = (E, kt * 128 // group, nt * 128)
+    stored, shape = _w4_shapes(E, N, K, group)
     with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():      # memory of the call's own stream
-        q, scale = w.new_empty((E, nt, kt, 128, 64), dtype=torch.uint8), w.new_empty(shape, dtype=torch.bfloat16)
+        q, scale = w.new_empty(stored, dtype=torch.uint8), w.new_empty(shape, dtype=torch.bfloat16)
         zero = None if symmetric else w.new_empty(shape, dtype=torch.uint8)
     pq, ps, pz = q.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr()
-    _enqueue("bls_w4_quantize", dev, w.data_ptr(), _DTYPE[w.dtype], ld, E, N, K, group, pq, ps, pz, _on(stream, dev))
+    _enqueue(lib().bls_w4_quantize, dev, w.data_ptr(), _DTYPE[w.dtype], ld, E, N, K, group, pq, ps, pz, _on(stream, dev))
     return W4._of((q, scale, zero), (E, N, K, group), (pq, ps, pz), dev)
 
 
@@ -695,7 +699,7 @@ def bls_w4_dequantize(w4: W4, w: torch.Tensor, stream: Optional[torch.cuda.Strea
     if (E, N, K) != w4._sizes[:3]:
         raise ValueError(f"w: expected {w4._sizes[:3]}")
     dev = _gpu(w, "w", stream)
-    _enqueue("bls_w4_dequantize", dev, *w4._args_on(dev), w.data_ptr(), _DTYPE[w.dtype], ld, _on(stream, dev))
+    _enqueue(lib().bls_w4_dequantize, dev, *w4._args_on(dev), w.data_ptr(), _DTYPE[w.dtype], ld, _on(stream, dev))
 
 
 _w4_status_word = {}                         # device number -> (int32 [1], its address), zeroed once: waits that gave up are latched here
@@ -746,6 +750,6 @@ def bls_w4_linear(w4: W4, x: torch.Tensor, y: torch.Tensor, offsets: Optional[to
         nbytes = size.value
         if nbytes:
             ws = _scratch(nbytes, stream, x)
-    _enqueue("bls_w4_linear", dev, *w4._args_on(dev), px, _dt(x, "x"), ldx, rows, _flat(offsets, "offsets", (E + 1,), _I32, dev),
+    _enqueue(lib().bls_w4_linear, dev, *w4._args_on(dev), px, _dt(x, "x"), ldx, rows, _flat(offsets, "offsets", (E + 1,), _I32, dev),
              _flat(bias, "bias", (E, N), _F32, dev), act, py, _dt(y, "y"), ldy, ws.data_ptr() if nbytes else None, nbytes,
              _status_word(dev)[1], _on(stream, dev))

@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) bls_moe_route_kernel(const int 
     for (int i = max(t0, scratch[31]) + threadIdx.x; i < t1; i += ROUTE_THREADS) order[i] = -1;
 }
 
-// Tiles of the slots, of 1024 slots at least; one up to ROUTE_ONE slots (one block and one launch: 4000 slots take 6.4 us, two
+// Tiles of the slots, of about 1024 slots at least (832 of 4097); one up to ROUTE_ONE slots (one block and one launch: 4000 slots take 6.4 us, two
 // kernels 5.4 us and another launch; 8000 slots 10.3 and 5.4).  74 tiles, half the SMs: every block reads the counts of all tiles, and
 // 400k slots over 256 experts take 13.7 us with 74 tiles, 18.3 with 148, 16.1 with 50.
 void route_tiles(long long n, int &tiles, int &tile)
@@ -272,7 +272,8 @@ __device__ __forceinline__ void zero_tail(const MoveArgs &m, const MoveLane &l, 
 }
 
 // A thread reads U pieces of a token and writes them to the token's k places: x is read once.  Bound by memory:
-// 16384 x 8 x 2048 bf16 in 100 us (6.0 TB/s).
+// 16384 x 8 x 2048 bf16 in 100 us (6.0 TB/s).  Rows that no whole piece divides (V = 1) are bound by issue: 75 % busy in
+// 3001 x 3 x 1531, fp32 or bf16.
 template <class T, int V>
 __global__ void __launch_bounds__(MOVE_THREADS) bls_moe_dispatch_kernel(const __grid_constant__ MoveArgs m)
 {
@@ -300,7 +301,8 @@ __global__ void __launch_bounds__(MOVE_THREADS) bls_moe_dispatch_kernel(const __
 }
 
 // A thread sums U pieces of a token over its k rows, several rows' pieces on their way at a time, in the order of the slots.
-// Bound by memory: 16384 x 8 x 2048 bf16 in 94 us (6.3 TB/s); eight rows on their way instead of four: 151.
+// Bound by memory: 16384 x 8 x 2048 bf16 in 94 us (6.3 TB/s); eight rows on their way instead of four: 151.  With V = 1 by
+// issue: 58 % busy with fp32, 66 % with bf16.
 template <class T, int V>
 __global__ void __launch_bounds__(MOVE_THREADS) bls_moe_combine_kernel(const __grid_constant__ MoveArgs m)
 {

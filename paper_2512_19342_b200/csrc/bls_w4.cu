@@ -11,8 +11,11 @@
 // At this size a layer is a few such steps per warp, so what counts is that all loads are on their way
 // at once and that many warps share the unpacking: the 16 warps of a block split K (and, where K is short
 // or there is plenty of work, also the outputs), and their sums meet in shared memory in the order of the slices.
-// One row: 4096 x 4096 in 5.5 us, 8192 x 8192 in 15 us (2.2 TB/s); 64 matrices of 2048 x 1024 with a row each in 25 us (2.7 TB/s).
-// The bound is the issue of instructions, 179 for 16 x 128 weights.
+// One row: 4096 x 4096 in 5.3 us, 8192 x 8192 in 15 us (2.2 TB/s); 64 matrices of 2048 x 1024 with a row each in 25 us (2.7 TB/s).
+// Neither memory (23 % of its rate, 8192 x 8192) nor issue (50 %; 7.5 M instructions are 6.4 of the 15 us) is full: a warp asks for its
+// next tiles only after it has used the ones it has, and the block meets twice a round for x.  So a round costs
+// a memory latency and then its instructions, 179 for 16 x 128 weights.
+// 64 registers per thread, for two blocks on an SM; 10 of the 12 forms spill 4 to 12 bytes of them.
 #include "bls_w4.cuh"
 #include "bls_w4_gemm.h"
 
@@ -436,8 +439,11 @@ bool w4_shape(int E, int N, int K, int group, W4Weights &w)
     return true;
 }
 
-// Which kernel: by the rows that a matrix gets on average.  4096 x 4096: 8 rows 6.9 us here, 9 rows 9.4 us in tiles and 10.2 here,
-// 16 rows 9.5 and 11.6; 8192 x 8192: 8 rows 20 us here, 16 rows 20 in tiles and 38 here.
+// Which kernel: by the rows that a matrix gets on average, since the offsets are on the device.  4096 x 4096: 8 rows 6.9 us here,
+// 9 rows 9.8 us in tiles and 10.2 here, 16 rows 9.8 and 11.6; 8192 x 8192: 8 rows 20 us here, 16 rows 20 in tiles and 38 here.
+// With many matrices the average is a fair guide for even loads alone.  64 matrices of 2048 x 1024 (groups of 64): 128 rows over
+// all of them take 26 us here and 39 in tiles, 512 rows 44 and 39; but 512 rows of 16, 4 and 1 of the matrices take 80, 188 and
+// 459 us here and 14, 14 and 9 in tiles, because a matrix's rows are taken eight at a time, one after the other.
 bool many_rows(const W4Weights &w, int64_t rows) { return rows > 8ll * w.E; }
 
 template <class T, int GROUP>
@@ -478,7 +484,6 @@ bls_status_t bls_w4_quantize(const void *w, int dtype, int64_t ldw, int E, int N
 {
     W4Weights d = {};
     if (!w || !q || !scale || ((uintptr_t)q & 15) || dtype < 0 || dtype > 2 || ldw < K || !w4_shape(E, N, K, group, d)) return BLS_EINVAL;
-    if (d.NT > 65535) return BLS_EINVAL;
     return launch_serialised(zero ? W4_PICK(bls_w4_quantize_kernel, dtype, w4_whole(w, dtype, ldw), W4_COMMA true) :
                                     W4_PICK(bls_w4_quantize_kernel, dtype, w4_whole(w, dtype, ldw), W4_COMMA false), dim3(d.KT, d.NT, E), dim3(256),
                              (cudaStream_t)cuda_stream, w, (long long)ldw, d, q,

@@ -11,8 +11,9 @@
 // With too few tiles for the SMs the CTAs of a cluster split K (SPLIT: one tile per cluster, the sums
 // meet through distributed shared memory in the order of the slices).
 //
-// Bound by the tensor cores with groups of 128 (8192 x 8192 x 4096 in 421 us, 1.31 PFLOP/s),
-// by scaling with groups of 64 and 32 (650 and 1120 us).
+// Bound by the tensor cores with groups of 128 (8192 x 8192 x 4096 in 432 us, 1.27 PFLOP/s),
+// by scaling with groups of 64 and 32 (622 to 640 and 1115 us; of 4096 x 4096 x 4096 the tensor pipe is busy for 59, 39 and 22 % of the
+// cycles with groups of 128, 64 and 32).  The forms with two halves spill 20 bytes of registers.
 //
 // Roles: warps 0-3 unpack, warps 4-11 scale and store, one thread of warp 12 loads (TMA for x, bulk
 // copies for the weight tile and its scales and zero points), one thread of warp 13 issues the
