@@ -58,25 +58,31 @@ def same(a, b):
 def test_scratch_memory_belongs_to_the_call_s_stream():
     """A call returns before its kernels run.  Memory that the caller takes then, on another stream, and clears must not be the call's own."""
     step, s = Step(1), torch.cuda.Stream()
-    step()
-    torch.cuda.synchronize()
-    want = step.results()
-    for t in (*step.routes, step.rows, step.y, step.out, step.dy, step.dw):
-        t.fill_(-3)
-    torch.cuda.synchronize()
     sizes = [1 << p for p in range(9, 23)] + [step.n * step.k * 264 * 2]
 
     def clear():
         for n in sizes:
             torch.zeros(n, dtype=torch.uint8, device="cuda")
 
-    with torch.cuda.stream(s):
-        torch.cuda._sleep(100_000_000)
-    step(s, clear)
-    clear()
-    assert not s.query()                                      # everything above was enqueued while the stream was held up
+    step()
+    want = step.results()
+    step(s, clear)                                            # the allocator has memory for all of it from here on, and asks the driver for none
     torch.cuda.synchronize()
-    assert same(step.results(), want) and bls.bls_w4_status() == bls.BLS_OK
+    held = False
+    for _ in range(3):
+        for t in (*step.routes, step.rows, step.y, step.out, step.dy, step.dw):
+            t.fill_(-3)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(400_000_000)                    # 0.2 s
+        step(s, clear)
+        clear()
+        held = held or not s.query()                          # everything was enqueued while the stream was held up
+        torch.cuda.synchronize()
+        assert same(step.results(), want)
+    assert bls.bls_w4_status() == bls.BLS_OK
+    if not held:
+        pytest.skip("the host was too slow to enqueue the calls within 0.2 s")
 
 
 def test_scratch_memory_in_a_cuda_graph():
